@@ -288,6 +288,151 @@ int osdn_step_host(const osdn_params* p, const void* q_host, const void* k_host,
  */
 int osdn_workspace_region(const osdn_params* p, int need_bwd, const char* name, size_t* offset, size_t* bytes);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators beside the layer.  A model block's q, k, v come out of a short causal convolution, its q
+ * and k are normalised per head (the layer expects unit keys; blocks with softmax attention beside it
+ * rotate them too), and a gated linear recurrence without keys is the other recurrent mixer that such
+ * models interleave.  The three share the conventions at the head of this file, with these additions:
+ *   - Token tensors are rows of channels, [tokens, C] row-major: tokens = B T (dense) or T (var-len,
+ *     B = 1).  A [T, H, D] tensor is C = H D channels.
+ *   - Var-len: sequences may be empty.  A batch may be padded behind its last sequence (cu[nseq] < T):
+ *     rows from cu[nseq] on are not read into any result and stay as they were in every output.  A
+ *     cu_seqlens that breaks its contract otherwise (cu[0] != 0, a decreasing pair, cu[nseq] > T) gives
+ *     undefined results, but no access leaves the tensors.
+ *   - Inputs are never written.  Outputs may not overlap inputs or one another unless stated.
+ *   - T >= 1, any number of channels >= 1 where nothing else is stated; B T <= 1e9 and B T C <= 2e10.
+ * ------------------------------------------------------------------------------------------- */
+
+/*
+ * Gated linear recurrence, channel by channel, with a state that is carried from call to call:
+ *     h_t = a_t h_{t-1} + b_t,   a_t = exp(gate_t),   b_t = x_t (OSDN_INPUT_PLAIN) or (1 - a_t) x_t
+ *     (OSDN_INPUT_COMPLEMENT, 1 - a_t without cancellation),   out_t = h_t.
+ * Log gates are <= 0 and fp32, as everywhere in this library; -inf is a factor of zero.  All arithmetic is
+ * fp32; a gate near one enters as its distance from one, so that memories of thousands of tokens keep
+ * their length.
+ */
+enum { OSDN_INPUT_PLAIN = 0, OSDN_INPUT_COMPLEMENT = 1 };
+typedef struct osdn_scan_params {
+    int32_t B, T, C;            /* dense: [B,T,C]; var-len: B = 1, T = packed tokens                  */
+    int32_t io_dtype;           /* of x, out, dout, dx: OSDN_FP32 | OSDN_BF16                         */
+    int32_t input_gate;         /* OSDN_INPUT_*                                                       */
+    int32_t nseq;               /* 0 = dense                                                          */
+    const int32_t* cu_seqlens;  /* device pointer, nseq+1 entries (var-len only)                      */
+    int32_t flags;              /* OSDN_FLAG_SAVE_RESIDUALS (fwd), OSDN_FLAG_RESIDUALS_VALID (bwd)    */
+} osdn_scan_params;
+
+/* Bytes of the workspace that connects a forward that saves residuals with its backward (the states at
+ * every 128th token, fp32); 0 on invalid params. */
+size_t osdn_scan_workspace_bytes(const osdn_scan_params* p);
+
+/*
+ *   in : x [tokens,C] io_dtype; gate [tokens,C] fp32; init_state [S,C] fp32 (NULL = zeros).
+ *   out: out [tokens,C] io_dtype; final_state [S,C] fp32 (may be NULL).
+ *   workspace: with OSDN_FLAG_SAVE_RESIDUALS osdn_scan_workspace_bytes(p) bytes, else not used (NULL).
+ */
+int osdn_scan_fwd(const osdn_scan_params* p, const void* x, const float* gate, const float* init_state,
+                  void* out, float* final_state, void* workspace, size_t workspace_bytes, void* cuda_stream);
+/*
+ * Gradients of sum(out*dout) + sum(final_state*dfinal_state).
+ *   in : the forward's inputs; dout [tokens,C] io_dtype; dfinal_state [S,C] fp32 (NULL = zeros).
+ *   out: dx [tokens,C] io_dtype; dgate [tokens,C] fp32; dinit_state [S,C] fp32 (may be NULL).
+ *   workspace: osdn_scan_workspace_bytes(p) bytes; with OSDN_FLAG_RESIDUALS_VALID it holds what the
+ *        forward saved (same params and inputs), otherwise the states are computed again.
+ */
+int osdn_scan_bwd(const osdn_scan_params* p, const void* x, const float* gate, const float* init_state,
+                  const void* dout, const float* dfinal_state, void* dx, float* dgate, float* dinit_state,
+                  void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* Recurrent (decode) step: the p->T new tokens of each of the p->B sequences, dense only.
+ *   in: x, gate;  in/out: state [B,C] fp32, updated in place;  out: out [B,T,C]. */
+int osdn_scan_step(const osdn_scan_params* p, const void* x, const float* gate, float* state, void* out,
+                   void* cuda_stream);
+
+/*
+ * Short causal depthwise convolution over the tokens of a sequence, W taps a channel (2, 3 or 4):
+ *     z_t = bias + sum_{i<W} weight_i x_{t-(W-1)+i},   out_t = z_t (OSDN_ACT_NONE) or z_t sigmoid(z_t)
+ *     (OSDN_ACT_SILU).
+ * The rows in front of a sequence are its state: the last W-1 input rows of what came before, oldest first.
+ */
+enum { OSDN_ACT_NONE = 0, OSDN_ACT_SILU = 1 };
+typedef struct osdn_conv_params {
+    int32_t B, T, C, W;
+    int32_t io_dtype;           /* of x, out, the states and their gradients                          */
+    int32_t activation;         /* OSDN_ACT_*                                                         */
+    int32_t nseq;
+    const int32_t* cu_seqlens;
+    int32_t flags;              /* none                                                               */
+} osdn_conv_params;
+
+/* Bytes of scratch of the backward (partial sums of the weights' gradients); 0 on invalid params. */
+size_t osdn_short_conv_workspace_bytes(const osdn_conv_params* p);
+/*
+ *   in : x [tokens,C]; weight [C,W], bias [C] fp32 (bias may be NULL); init_state [S,W-1,C] (NULL = zeros).
+ *   out: out [tokens,C]; final_state [S,W-1,C] (may be NULL).
+ */
+int osdn_short_conv_fwd(const osdn_conv_params* p, const void* x, const float* weight, const float* bias,
+                        const void* init_state, void* out, void* final_state, void* cuda_stream);
+/*
+ * Gradients of sum(out*dout) + sum(final_state*dfinal_state); the pre-activations are computed again.
+ *   out: dx [tokens,C]; dweight [C,W] fp32; dbias [C] fp32 (may be NULL); dinit_state [S,W-1,C] (may be NULL).
+ *   The sums over tokens are taken in an order that the shape alone decides.
+ */
+int osdn_short_conv_bwd(const osdn_conv_params* p, const void* x, const float* weight, const float* bias,
+                        const void* init_state, const void* dout, const void* dfinal_state, void* dx,
+                        float* dweight, float* dbias, void* dinit_state, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream);
+/* Recurrent (decode) step over the p->T new tokens of each of the p->B sequences, dense only.
+ *   in/out: state [B,W-1,C], updated in place. */
+int osdn_short_conv_step(const osdn_conv_params* p, const void* x, const float* weight, const float* bias,
+                         void* state, void* out, void* cuda_stream);
+
+/*
+ * Norms of the queries and the keys, head by head, with the rotation by the position in the same pass:
+ *     u = x r,   r = (|x|^2 + eps)^-1/2 (OSDN_NORM_L2) or (|x|^2 / D + eps)^-1/2 (OSDN_NORM_RMS),
+ *     y = Rot_pos(u * weight),   the pair n of the first rot_dim features turned by the angle pos inv_freq_n.
+ * A pair is (n, n + rot_dim/2) (OSDN_ROT_HALF) or (2n, 2n + 1) (OSDN_ROT_PAIRS).  Angles are reduced in
+ * 64 bits, so that far positions turn by what near ones do.  Single new tokens (decode) are this call with
+ * their positions.
+ * D: a multiple of 8, 8 to 256; rot_dim: 0 or a multiple of 16 up to D.  q and k may be parts of wider rows
+ * (a fused projection): q_row and k_row are the elements from one token to the next, a multiple of 16 bytes
+ * and at least Hq D (Hk D); 0 = packed.  dq_row and dk_row are those of the gradients dq and dk.  q_out, k_out and their
+ * gradients are packed.  |x|^2 is summed in fp32 and has to be finite there.
+ */
+enum { OSDN_NORM_L2 = 0, OSDN_NORM_RMS = 1 };
+enum { OSDN_ROT_HALF = 0, OSDN_ROT_PAIRS = 1 };
+typedef struct osdn_qk_norm_params {
+    int32_t B, T, Hq, Hk, D;
+    int32_t io_dtype;           /* of q, k, q_out, k_out and their gradients                          */
+    int32_t norm, rot_dim, rot_layout;
+    float   eps;                /* > 0                                                                */
+    int32_t nseq;               /* 0 = dense                                                          */
+    const int32_t* cu_seqlens;
+    int32_t flags;              /* none                                                               */
+    int64_t q_row, k_row, dq_row, dk_row;
+} osdn_qk_norm_params;
+
+/* Bytes of scratch of the backward (partial sums of the weights' gradients); 0 on invalid params. */
+size_t osdn_qk_norm_workspace_bytes(const osdn_qk_norm_params* p);
+/*
+ *   in : q [tokens,Hq,D], k [tokens,Hk,D]; q_weight, k_weight [D] fp32 (NULL = ones); inv_freq
+ *        [rot_dim/2] fp64, radians a position (required with rot_dim > 0); positions [tokens] int32 (NULL:
+ *        the place in the token's sequence).
+ *   out: q_out, k_out: packed; may be q and k themselves where those are packed.
+ */
+int osdn_qk_norm_fwd(const osdn_qk_norm_params* p, const void* q, const void* k, const float* q_weight,
+                     const float* k_weight, const double* inv_freq, const int32_t* positions, void* q_out,
+                     void* k_out, void* cuda_stream);
+/*
+ *   in : the forward's inputs; dq_out, dk_out.
+ *   out: dq, dk (may be dq_out and dk_out themselves where packed); dq_weight, dk_weight [D] fp32 (may be NULL;
+ *        require the weight).
+ *   The sums over tokens and heads are taken in an order that the shape alone decides.
+ *   workspace: osdn_qk_norm_workspace_bytes(p) bytes where a weight's gradient is asked for, else NULL.
+ */
+int osdn_qk_norm_bwd(const osdn_qk_norm_params* p, const void* q, const void* k, const float* q_weight,
+                     const float* k_weight, const double* inv_freq, const int32_t* positions,
+                     const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
+                     float* dk_weight, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Reads the device status word at the head of a workspace (synchronous 4-byte copy).
  * 0 = no device-side error recorded. */
 int osdn_read_device_status(const void* workspace, int32_t* status_host);
@@ -305,8 +450,7 @@ int osdn_selftest_wait_timeout(void* workspace, uint32_t limit_us, void* cuda_st
 
 const char* osdn_status_string(int status);
 
-/* Number of kernel launches the most recent osdn_fwd / osdn_bwd / osdn_precond_update call of
- * this thread enqueued (for launch accounting in benchmarks). */
+/* Number of kernel launches the most recent call of this thread that computes something enqueued (for launch accounting in benchmarks). */
 int osdn_last_launch_count(void);
 
 /*

@@ -7,15 +7,34 @@ fallback: if the library is missing or no CUDA device is present the calls raise
     from paper_2605_13473_b200 import osdn_fwd, osdn_bwd, osdn_precond_update
 """
 from .binding import (  # noqa: F401
+    FLAG_RESIDUALS_VALID,
+    FLAG_SAVE_RESIDUALS,
+    ConvParams,
     OsdnParams,
+    QkNormParams,
+    ScanParams,
     load_library,
+    make_conv_params,
     make_params,
+    make_qk_norm_params,
+    make_scan_params,
     osdn_bwd,
     osdn_fwd,
     osdn_fwd_static,
     osdn_decode_step,
     osdn_precond_update,
     osdn_residual_ratio,
+    osdn_qk_norm_bwd,
+    osdn_qk_norm_fwd,
+    osdn_qk_norm_workspace_bytes,
+    osdn_scan_bwd,
+    osdn_scan_fwd,
+    osdn_scan_step,
+    osdn_scan_workspace_bytes,
+    osdn_short_conv_bwd,
+    osdn_short_conv_fwd,
+    osdn_short_conv_step,
+    osdn_short_conv_workspace_bytes,
     osdn_step_host,
     osdn_workspace_bytes,
     osdn_host_staging_bytes,

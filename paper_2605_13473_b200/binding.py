@@ -21,6 +21,9 @@ EXPORTS = [
     "osdn_stage_timing_enable", "osdn_stage_timing_read", "osdn_workspace_region",
     "osdn_fwd_static", "osdn_decode_step", "osdn_residual_ratio", "osdn_read_static_status",
     "osdn_selftest_wait_timeout", "osdn_kda_workspace_bytes", "osdn_kda_fwd", "osdn_kda_bwd",
+    "osdn_scan_workspace_bytes", "osdn_scan_fwd", "osdn_scan_bwd", "osdn_scan_step",
+    "osdn_short_conv_workspace_bytes", "osdn_short_conv_fwd", "osdn_short_conv_bwd", "osdn_short_conv_step",
+    "osdn_qk_norm_workspace_bytes", "osdn_qk_norm_fwd", "osdn_qk_norm_bwd",
 ]
 
 
@@ -32,6 +35,35 @@ class OsdnParams(ctypes.Structure):
         ("eps", ctypes.c_float), ("scale", ctypes.c_float),
         ("beta_aware", ctypes.c_int32), ("apf_mode", ctypes.c_int32), ("clamp", ctypes.c_int32),
         ("nseq", ctypes.c_int32), ("cu_seqlens", ctypes.c_void_p), ("flags", ctypes.c_int32),
+    ]
+
+
+class ScanParams(ctypes.Structure):
+    """osdn_scan_params; see ``make_scan_params``."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("C", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+        ("input_gate", ctypes.c_int32), ("nseq", ctypes.c_int32), ("cu_seqlens", ctypes.c_void_p),
+        ("flags", ctypes.c_int32),
+    ]
+
+
+class ConvParams(ctypes.Structure):
+    """osdn_conv_params; see ``make_conv_params``."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("C", ctypes.c_int32), ("W", ctypes.c_int32),
+        ("io_dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("nseq", ctypes.c_int32),
+        ("cu_seqlens", ctypes.c_void_p), ("flags", ctypes.c_int32),
+    ]
+
+
+class QkNormParams(ctypes.Structure):
+    """osdn_qk_norm_params; see ``make_qk_norm_params``."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32),
+        ("D", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+        ("rot_layout", ctypes.c_int32), ("eps", ctypes.c_float), ("nseq", ctypes.c_int32),
+        ("cu_seqlens", ctypes.c_void_p), ("flags", ctypes.c_int32), ("q_row", ctypes.c_int64),
+        ("k_row", ctypes.c_int64), ("dq_row", ctypes.c_int64), ("dk_row", ctypes.c_int64),
     ]
 
 
@@ -69,6 +101,16 @@ def load_library(path: Optional[str] = None):
     lib.osdn_kda_fwd.argtypes = [pp] + [vp] * 11 + [vp, sz, vp]
     lib.osdn_kda_bwd.restype = ci
     lib.osdn_kda_bwd.argtypes = [pp] + [vp] * 19 + [vp, sz, vp]
+    sp, cp, np_ = ctypes.POINTER(ScanParams), ctypes.POINTER(ConvParams), ctypes.POINTER(QkNormParams)
+    for name, args in (("osdn_scan_fwd", [sp] + [vp] * 6 + [sz, vp]), ("osdn_scan_bwd", [sp] + [vp] * 9 + [sz, vp]),
+                       ("osdn_scan_step", [sp] + [vp] * 5), ("osdn_short_conv_fwd", [cp] + [vp] * 7),
+                       ("osdn_short_conv_bwd", [cp] + [vp] * 11 + [sz, vp]), ("osdn_short_conv_step", [cp] + [vp] * 6),
+                       ("osdn_qk_norm_fwd", [np_] + [vp] * 9), ("osdn_qk_norm_bwd", [np_] + [vp] * 13 + [sz, vp])):
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = args
+    for name, params in (("osdn_scan", sp), ("osdn_short_conv", cp), ("osdn_qk_norm", np_)):
+        getattr(lib, name + "_workspace_bytes").restype = sz
+        getattr(lib, name + "_workspace_bytes").argtypes = [params]
     lib.osdn_step_host.restype = ci
     lib.osdn_step_host.argtypes = [pp] + [vp] * 12 + [vp, sz, vp]
     lib.osdn_read_device_status.restype = ci
@@ -94,7 +136,8 @@ def load_library(path: Optional[str] = None):
 
 # The hot calls go through the extension module _osdn_call (csrc/call.cpp), which turns tensors into pointers
 # natively; the numbers are its table of calls.
-_FWD, _BWD, _KDA_FWD, _KDA_BWD, _PRECOND, _RATIO, _DECODE, _FWD_STATIC = range(8)
+(_FWD, _BWD, _KDA_FWD, _KDA_BWD, _PRECOND, _RATIO, _DECODE, _FWD_STATIC, _SCAN_FWD, _SCAN_BWD, _SCAN_STEP, _CONV_FWD,
+ _CONV_BWD, _CONV_STEP, _NORM_FWD, _NORM_BWD) = range(16)
 
 
 def _call(*args) -> int:
@@ -106,7 +149,7 @@ def _call(*args) -> int:
     except ImportError as e:
         raise RuntimeError("the extension module _osdn_call is missing or does not load: build it first "
                            "(python paper_2605_13473_b200/build.py); there is no fallback path") from e
-    register(OsdnParams)
+    register(OsdnParams, ScanParams, ConvParams, QkNormParams)
     _call = call
     return call(*args)
 
@@ -289,6 +332,101 @@ def osdn_step_host(p: OsdnParams, q, k, v, beta, gate, dout, out, dq, dk, dv, db
                             _ptr(out), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbeta), _ptr(dgate), _ptr(staging),
                             staging.nbytes, _stream_ptr())
     _check(rc, "osdn_step_host")
+
+
+# ---------------------------------------------------------------------------------------------
+# Operators beside the layer: the gated linear recurrence, the short causal convolution, the norms of queries and
+# keys.  Shapes and meanings: include/osdn.h.  Tensors have to be on the current CUDA device, of the dtype and size that
+# the params say, and contiguous (q, k, dq, dk: rows as the params say); a ValueError tells which one is not.
+# ---------------------------------------------------------------------------------------------
+def _batch(p, B, T, io_dtype, cu_seqlens, flags):
+    p.B, p.T, p.io_dtype, p.flags = B, T, {"fp32": 0, "bf16": 1}[io_dtype], flags
+    if cu_seqlens is not None:
+        if cu_seqlens.dtype != torch.int32 or not cu_seqlens.is_cuda or not cu_seqlens.is_contiguous() or cu_seqlens.numel() < 2:
+            raise ValueError("cu_seqlens: nseq + 1 contiguous int32 entries on the GPU")
+        p.nseq, p.cu_seqlens = cu_seqlens.numel() - 1, cu_seqlens.data_ptr()
+        p._cu_seqlens = cu_seqlens   # alive as long as the params
+    return p
+
+
+def make_scan_params(*, B: int, T: int, C: int, io_dtype: str, input_gate: str = "plain",
+                     cu_seqlens: Optional[torch.Tensor] = None, flags: int = 0) -> ScanParams:
+    """Gated linear recurrence over C channels; ``input_gate``: "plain" (b = x) or "complement" (b = (1 - a) x)."""
+    p = ScanParams()
+    p.C, p.input_gate = C, {"plain": 0, "complement": 1}[input_gate]
+    return _batch(p, B, T, io_dtype, cu_seqlens, flags)
+
+
+def make_conv_params(*, B: int, T: int, C: int, W: int, io_dtype: str, activation: str = "silu",
+                     cu_seqlens: Optional[torch.Tensor] = None, flags: int = 0) -> ConvParams:
+    """Causal depthwise convolution of W taps over C channels; ``activation``: "silu" or "none"."""
+    p = ConvParams()
+    p.C, p.W, p.activation = C, W, {"none": 0, "silu": 1}[activation]
+    return _batch(p, B, T, io_dtype, cu_seqlens, flags)
+
+
+def make_qk_norm_params(*, B: int, T: int, Hq: int, Hk: int, D: int, io_dtype: str, norm: str = "l2", eps: float = 1e-6,
+                        rot_dim: int = 0, rot_layout: str = "half", cu_seqlens: Optional[torch.Tensor] = None,
+                        q_row: int = 0, k_row: int = 0, dq_row: int = 0, dk_row: int = 0, flags: int = 0) -> QkNormParams:
+    """Norms of Hq query and Hk key heads of size D; ``norm``: "l2" or "rms"; ``rot_layout``: "half" or "pairs";
+    ``*_row``: elements from one token to the next where a tensor is part of wider rows (its ``stride(0)``)."""
+    p = QkNormParams()
+    p.Hq, p.Hk, p.D, p.eps = Hq, Hk, D, eps
+    p.norm, p.rot_dim, p.rot_layout = {"l2": 0, "rms": 1}[norm], rot_dim, {"half": 0, "pairs": 1}[rot_layout]
+    p.q_row, p.k_row, p.dq_row, p.dk_row = q_row, k_row, dq_row, dk_row
+    return _batch(p, B, T, io_dtype, cu_seqlens, flags)
+
+
+def osdn_scan_workspace_bytes(p: ScanParams) -> int:
+    return int(load_library().osdn_scan_workspace_bytes(ctypes.byref(p)))
+
+
+def osdn_scan_fwd(p: ScanParams, x, gate, init_state, out, final_state, workspace=None):
+    """``workspace``: with FLAG_SAVE_RESIDUALS, what osdn_scan_bwd is given afterwards."""
+    _check(_call(_SCAN_FWD, p, x, gate, init_state, out, final_state, workspace), "osdn_scan_fwd")
+
+
+def osdn_scan_bwd(p: ScanParams, x, gate, init_state, dout, dfinal_state, dx, dgate, dinit_state, workspace):
+    _check(_call(_SCAN_BWD, p, x, gate, init_state, dout, dfinal_state, dx, dgate, dinit_state, workspace), "osdn_scan_bwd")
+
+
+def osdn_scan_step(p: ScanParams, x, gate, state, out):
+    """``state`` [B,C] fp32 is updated in place."""
+    _check(_call(_SCAN_STEP, p, x, gate, state, out), "osdn_scan_step")
+
+
+def osdn_short_conv_workspace_bytes(p: ConvParams) -> int:
+    return int(load_library().osdn_short_conv_workspace_bytes(ctypes.byref(p)))
+
+
+def osdn_short_conv_fwd(p: ConvParams, x, weight, bias, init_state, out, final_state):
+    _check(_call(_CONV_FWD, p, x, weight, bias, init_state, out, final_state), "osdn_short_conv_fwd")
+
+
+def osdn_short_conv_bwd(p: ConvParams, x, weight, bias, init_state, dout, dfinal_state, dx, dweight, dbias, dinit_state,
+                        workspace):
+    _check(_call(_CONV_BWD, p, x, weight, bias, init_state, dout, dfinal_state, dx, dweight, dbias, dinit_state, workspace),
+           "osdn_short_conv_bwd")
+
+
+def osdn_short_conv_step(p: ConvParams, x, weight, bias, state, out):
+    """``state`` [B,W-1,C] (the last W-1 inputs, oldest first) is updated in place."""
+    _check(_call(_CONV_STEP, p, x, weight, bias, state, out), "osdn_short_conv_step")
+
+
+def osdn_qk_norm_workspace_bytes(p: QkNormParams) -> int:
+    return int(load_library().osdn_qk_norm_workspace_bytes(ctypes.byref(p)))
+
+
+def osdn_qk_norm_fwd(p: QkNormParams, q, k, q_weight, k_weight, inv_freq, positions, q_out, k_out):
+    _check(_call(_NORM_FWD, p, q, k, q_weight, k_weight, inv_freq, positions, q_out, k_out), "osdn_qk_norm_fwd")
+
+
+def osdn_qk_norm_bwd(p: QkNormParams, q, k, q_weight, k_weight, inv_freq, positions, dq_out, dk_out, dq, dk, dq_weight,
+                     dk_weight, workspace=None):
+    """``workspace`` is used only where dq_weight or dk_weight is asked for."""
+    _check(_call(_NORM_BWD, p, q, k, q_weight, k_weight, inv_freq, positions, dq_out, dk_out, dq, dk, dq_weight, dk_weight,
+                 workspace), "osdn_qk_norm_bwd")
 
 
 # ---------------------------------------------------------------------------------------------

@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libosdn.so")
 # python module: argument marshalling of the hot calls.  Its name carries the interpreter's ABI, so that another one does
 # not load it.
 CALL_LIB = os.path.join(HERE, "_osdn_call" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ["osdn_api.cu", "osdn_phase1.cu", "osdn_simt.cu", "osdn_tc.cu", "osdn_decode.cu", "osdn_kda.cu"]
+SOURCES = ["osdn_api.cu", "osdn_phase1.cu", "osdn_simt.cu", "osdn_tc.cu", "osdn_decode.cu", "osdn_kda.cu",
+           "osdn_rows_api.cu", "osdn_scan.cu", "osdn_conv.cu", "osdn_qk_norm.cu"]
 
 
 def _newest(paths):

@@ -100,6 +100,7 @@ int run_forward(const osdn_params& p, const Hyper& hy, const WsLayout& L, void* 
 namespace osdn {
 void stage_mark(cudaStream_t st, const char* name) { timer_push(st, name); }
 void stage_end(cudaStream_t st) { timer_push(st, nullptr); }
+int& last_launches() { return g_last_launches; }
 }  // namespace osdn
 
 extern "C" {

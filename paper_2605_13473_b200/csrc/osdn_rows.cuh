@@ -1,0 +1,133 @@
+// Device helpers of the operators on rows of channels: the recurrence, the convolution, the norms.
+#pragma once
+
+#include <algorithm>
+#include <type_traits>
+
+#include "osdn_common.cuh"
+
+namespace osdn {
+
+// Sequences of a batch of rows.  Dense: S sequences of T rows; packed (cu != nullptr): rows cu[s] .. cu[s+1]-1 of T.
+struct Rows {
+    const int* cu;
+    int S, T;
+};
+
+// First row behind the last sequence, and never behind the tensor.
+__device__ __forceinline__ int rows_end(const Rows& r) { return min(max(r.cu[r.S], 0), r.T); }
+
+// The last sequence that begins at or before row t (packed; 0 <= t < cu[S]), so not an empty one where t lies in a sequence.
+// Whatever cu holds, the result is one of 0 .. S-1.
+__device__ __forceinline__ int seq_of(const Rows& r, int t)
+{
+    int lo = 0, hi = r.S;   // cu[lo] <= t < cu[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (r.cu[mid] <= t) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// N consecutive channels as fp32; p is aligned to their size.
+template <int N> __device__ __forceinline__ void load_vec(const float* p, float (&x)[N])
+{
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const float4 v = reinterpret_cast<const float4*>(p)[i];
+            x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = p[i];
+    }
+}
+__device__ __forceinline__ float2 bf16_pair(uint32_t v)
+{
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t pair_bf16(float a, float b)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <int N> __device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&x)[N])
+{
+    if constexpr (N % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = bf16_pair(w[j]);
+                x[8 * i + 2 * j] = f.x; x[8 * i + 2 * j + 1] = f.y;
+            }
+        }
+    } else if constexpr (N == 4) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        const float2 a = bf16_pair(v.x), b = bf16_pair(v.y);
+        x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = __bfloat162float(p[i]);
+    }
+}
+template <int N> __device__ __forceinline__ void store_vec(float* p, const float (&x)[N])
+{
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i)
+            reinterpret_cast<float4*>(p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = x[i];
+    }
+}
+template <int N> __device__ __forceinline__ void store_vec(__nv_bfloat16* p, const float (&x)[N])
+{
+    if constexpr (N % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i)
+            reinterpret_cast<uint4*>(p)[i] = make_uint4(pair_bf16(x[8 * i], x[8 * i + 1]), pair_bf16(x[8 * i + 2], x[8 * i + 3]),
+                                                        pair_bf16(x[8 * i + 4], x[8 * i + 5]), pair_bf16(x[8 * i + 6], x[8 * i + 7]));
+    } else if constexpr (N == 4) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pair_bf16(x[0], x[1]), pair_bf16(x[2], x[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = __float2bfloat16_rn(x[i]);
+    }
+}
+
+inline int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// Entry points of the kernels' files.  The number of launches, or -1 on a launch error.
+int scan_forward(const osdn_scan_params& p, const void* x, const float* gate, const float* init, void* out, float* fin,
+                 void* ws, cudaStream_t st);
+int scan_backward(const osdn_scan_params& p, const void* x, const float* gate, const float* init, const void* dout,
+                  const float* dfin, void* dx, float* dgate, float* dinit, void* ws, cudaStream_t st);
+int scan_step(const osdn_scan_params& p, const void* x, const float* gate, float* state, void* out, cudaStream_t st);
+size_t scan_workspace(const osdn_scan_params& p);
+int conv_forward(const osdn_conv_params& p, const void* x, const float* w, const float* bias, const void* init, void* out,
+                 void* fin, cudaStream_t st);
+int conv_backward(const osdn_conv_params& p, const void* x, const float* w, const float* bias, const void* init,
+                  const void* dout, const void* dfin, void* dx, float* dw, float* dbias, void* dinit, void* ws, cudaStream_t st);
+int conv_step(const osdn_conv_params& p, const void* x, const float* w, const float* bias, void* state, void* out, cudaStream_t st);
+size_t conv_workspace(const osdn_conv_params& p);
+int qk_norm_forward(const osdn_qk_norm_params& p, const void* q, const void* k, const float* qw, const float* kw,
+                    const double* inv_freq, const int* pos, void* qo, void* ko, cudaStream_t st);
+int qk_norm_backward(const osdn_qk_norm_params& p, const void* q, const void* k, const float* qw, const float* kw,
+                     const double* inv_freq, const int* pos, const void* dqo, const void* dko, void* dq, void* dk, float* dqw,
+                     float* dkw, void* ws, cudaStream_t st);
+size_t qk_norm_workspace(const osdn_qk_norm_params& p);
+
+// Sums of the rows of part [G, M], in a fixed order: column m goes to out0[(m % C) W + m / C] where m < W C, else to
+// out1[m - W C]; either may be NULL.
+bool launch_sum_rows(const float* part, int G, int C, int W, int M, float* out0, float* out1, cudaStream_t st);
+
+// Launch count of the calling thread's last call (osdn_last_launch_count).
+int& last_launches();
+
+}  // namespace osdn
