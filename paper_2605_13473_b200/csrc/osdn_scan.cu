@@ -3,40 +3,108 @@
 
 #include "osdn_rows.cuh"
 
+#ifndef XCTA
+#define XCTA 120
+#endif
+#ifndef XW
+#define XW 16
+#endif
+#ifndef XFMIN
+#define XFMIN 16
+#endif
+#ifndef XBMIN
+#define XBMIN 16
+#endif
 namespace osdn {
 namespace {
 
-constexpr int TILE = 128;   // tokens between two states that the forward keeps for the backward
+constexpr int UNIT = 8;   // rows that a warp takes at a time; the forward keeps the state in front of each such stretch for the backward
 
-// exp(g) for g <= 0 in a form that keeps its distance from one.  Range reduction by powers of two (Cody and Waite:
-// g = n ln 2 + r with ln 2 in two floats), expm1(r) by its Taylor series to r^7 (|r| <= 0.347: remainder below 2e-8 of r).
-//   n = 0:  sign bit set, a = 1 + v, v = expm1(g), accurate relative to itself;
-//   else:   sign bit clear, a = v.
-// Stored as a rounded factor instead, a gate of -3e-4 keeps 1 - a to 1e-4 only, and the product of thousands of them
-// drifts.  Factors below 2^-126 are zero.
-struct Decay {
-    float v;
-    __device__ __forceinline__ static Decay of(float g)
-    {
-        g = g < -100.f ? -100.f : g;   // -inf too; a NaN stays one
-        const float t = fmaf(g, 1.44269504f, 12582912.f);   // 1.5 * 2^23: the sum's low bits are round(g / ln 2)
-        const float n = t - 12582912.f;
-        float r = fmaf(n, -0.693147182f, g);
-        r = fmaf(n, 1.90465421e-9f, r);                      // float(ln 2) - ln 2
-        float q = fmaf(r, 1.f / 5040, 1.f / 720);
-        q = fmaf(r, q, 1.f / 120);
-        q = fmaf(r, q, 1.f / 24);
-        q = fmaf(r, q, 1.f / 6);
-        q = fmaf(r, q, 0.5f);
-        const float p = fmaf(r * r, q, r);
-        const float scale = __int_as_float((__float_as_int(t) << 23) + 0x3f800000);   // 2^n
-        const float whole = n < -126.f ? 0.f : fmaf(p, scale, scale);
-        return {n == 0.f && g <= 0.f ? -fabsf(p) : whole};
+// N channels at once; two go through the packed fp32 instructions.
+template <int N> struct F {
+    float x[N];
+};
+__device__ __forceinline__ unsigned long long pack(const F<2>& a)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x[0]), "f"(a.x[1]));
+    return r;
+}
+__device__ __forceinline__ F<2> unpack(unsigned long long r)
+{
+    F<2> a;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a.x[0]), "=f"(a.x[1]) : "l"(r));
+    return a;
+}
+template <int N> __device__ __forceinline__ F<N> all(float v)
+{
+    F<N> a;
+#pragma unroll
+    for (int k = 0; k < N; ++k) a.x[k] = v;
+    return a;
+}
+template <int N> __device__ __forceinline__ F<N> fma(const F<N>& a, const F<N>& b, const F<N>& c)
+{
+    if constexpr (N == 2) {
+        unsigned long long d;
+        asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)), "l"(pack(c)));
+        return unpack(d);
+    } else {
+        return {{fmaf(a.x[0], b.x[0], c.x[0])}};
     }
-    __device__ __forceinline__ bool near_one() const { return __float_as_int(v) < 0; }
-    __device__ __forceinline__ float complement() const { return near_one() ? -v : 1.f - v; }
-    __device__ __forceinline__ float times(float y) const { return fmaf(v, y, near_one() ? y : 0.f); }
-    __device__ __forceinline__ float step(float h, float b) const { return fmaf(v, h, near_one() ? h + b : b); }   // a h + b
+}
+template <int N> __device__ __forceinline__ F<N> add(const F<N>& a, const F<N>& b)
+{
+    if constexpr (N == 2) {
+        unsigned long long d;
+        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)));
+        return unpack(d);
+    } else {
+        return {{a.x[0] + b.x[0]}};
+    }
+}
+template <int N> __device__ __forceinline__ F<N> mul(const F<N>& a, const F<N>& b)
+{
+    if constexpr (N == 2) {
+        unsigned long long d;
+        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)));
+        return unpack(d);
+    } else {
+        return {{a.x[0] * b.x[0]}};
+    }
+}
+
+// exp(g) for g <= 0 as the sum of two floats, hi the nearest one to it:
+//   |g| <= 1/4:  from expm1(g) by its Taylor series to g^6 (remainder below 5e-8 of it): the sum keeps the distance from one;
+//   else:        hi alone, by the hardware's exponential (2^-22 of a; a <= 0.78 forgets it within a few tokens); -inf is zero.
+// As one rounded factor, a gate of -3e-4 keeps 1 - a to 1e-4 only, and a product of thousands of them drifts.  Two floats cost
+// one packed fma more a step and no selection (with the form chosen at every step: 38 instructions an element against 22).
+template <int N> struct Decay {
+    F<N> hi, lo;
+    __device__ __forceinline__ static Decay of(const F<N>& g)
+    {
+        F<N> q = fma(g, all<N>(1.f / 720), all<N>(1.f / 120));
+        q = fma(g, q, all<N>(1.f / 24));
+        q = fma(g, q, all<N>(1.f / 6));
+        q = fma(g, q, all<N>(0.5f));
+        const F<N> p = fma(mul(g, g), q, g);
+        const F<N> e = mul(g, all<N>(1.44269504f));
+        const F<N> near = add(p, all<N>(1.f));
+        const F<N> rest = add(p, fma(near, all<N>(-1.f), all<N>(1.f)));   // p - (near - 1), exact
+        Decay d;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float w;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(e.x[k]));
+            const bool is = fabsf(g.x[k]) <= 0.25f;
+            d.hi.x[k] = is ? near.x[k] : w;
+            d.lo.x[k] = is ? rest.x[k] : 0.f;
+        }
+        return d;
+    }
+    __device__ __forceinline__ F<N> complement() const { return fma(lo, all<N>(-1.f), fma(hi, all<N>(-1.f), all<N>(1.f))); }   // 1 - a
+    __device__ __forceinline__ F<N> times(const F<N>& y) const { return fma(hi, y, mul(lo, y)); }                    // a y
+    __device__ __forceinline__ F<N> step(const F<N>& h, const F<N>& b) const { return fma(hi, h, fma(lo, h, b)); }   // a h + b
 };
 
 struct ScanArgs {
@@ -44,95 +112,139 @@ struct ScanArgs {
     const float *gate, *init, *dfin;
     void *out, *dx;
     float *fin, *dgate, *dinit;
-    float* saved;    // [tiles, C] (dense: [S, tiles, C]) state in front of every TILE-th row
+    float* saved;    // [units, C] (dense: [S, units, C]) state in front of every UNIT-th row
     const int* cu;   // packed rows; else sequence s of a flat batch begins at row s T
     int S, T;        // sequences; rows of a dense sequence, or all packed rows
     int C, rows;     // rows of a walk: a dense sequence's, or the whole flat batch's
-    int tiles, span; // tiles of a walk; CTAs that share it
+    int units, span; // units of a walk; CTAs that share it
     __device__ __forceinline__ int begin(int s) const { return cu ? cu[s] : s * T; }
 };
 
-// How a CTA covers a tile of TILE rows: groups of LANES threads side by side over LANES * VEC channels, each group TPG rows.
-template <typename T_, int VEC_, int LANES_, int THREADS_> struct Cover {
+// How a CTA covers its rows: its warps take units in turn, over CB channels, VEC to a lane.
+template <typename T_, int VEC_, int WARPS_> struct Cover {
     using T = T_;
-    static constexpr int VEC = VEC_, LANES = LANES_, THREADS = THREADS_, WARPS = THREADS / 32, PER_WARP = 32 / LANES;
-    static constexpr int CB = LANES * VEC, TPG = TILE * LANES / THREADS;
-    static constexpr bool STAGED = VEC == 4;   // the next tile is on its way in shared memory while this one is computed
+    static constexpr int VEC = VEC_, WARPS = WARPS_, CB = 32 * VEC, TPG = UNIT;
+    static constexpr bool STAGED = VEC == 2;   // a warp's next unit is on its way in shared memory while it computes one
 };
 constexpr int MAX_SPAN = 16;
 
 // VEC elements as they come from memory
 template <typename T, int VEC> struct Raw;
-template <> struct Raw<float, 4> {
-    float4 v;
-    __device__ __forceinline__ float get(int k) const { return k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w; }
+template <> struct Raw<float, 2> {
+    float2 v;
+    __device__ __forceinline__ F<2> get() const { return {{v.x, v.y}}; }
 };
-template <> struct Raw<__nv_bfloat16, 4> {
-    uint2 v;
-    __device__ __forceinline__ float get(int k) const
-    {
-        const uint32_t w = k < 2 ? v.x : v.y;
-        return __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16);
-    }
+template <> struct Raw<__nv_bfloat16, 2> {
+    uint32_t v;
+    __device__ __forceinline__ F<2> get() const { return {{__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)}}; }
 };
 template <typename T> struct Raw<T, 1> {
     T v;
-    __device__ __forceinline__ float get(int) const { return ldf(&v); }
+    __device__ __forceinline__ F<1> get() const { return {{ldf(&v)}}; }
 };
-
-template <int BYTES> __device__ __forceinline__ void copy_async(void* smem, const void* src, bool real)
+template <int N> __device__ __forceinline__ F<N> read(const float* p)
 {
-    const uint32_t to = (uint32_t)__cvta_generic_to_shared(smem);
-    const int n = real ? BYTES : 0;   // the rest is filled with zeros
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(n) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(to), "l"(src), "r"(n), "n"(BYTES) : "memory");
+    if constexpr (N == 2) {
+        const float2 v = *reinterpret_cast<const float2*>(p);
+        return {{v.x, v.y}};
+    } else {
+        return {{*p}};
+    }
+}
+template <int N> __device__ __forceinline__ F<N> read_or_zero(const float* p, size_t at) { return p ? read<N>(p + at) : all<N>(0.f); }
+template <int N> __device__ __forceinline__ void write(float* p, const F<N>& a)
+{
+    if constexpr (N == 2) *reinterpret_cast<float2*>(p) = make_float2(a.x[0], a.x[1]);
+    else *p = a.x[0];
+}
+template <int N> __device__ __forceinline__ void write(__nv_bfloat16* p, const F<N>& a)
+{
+    if constexpr (N == 2) *reinterpret_cast<uint32_t*>(p) = pair_bf16(a.x[0], a.x[1]);
+    else *p = __float2bfloat16_rn(a.x[0]);
+}
+
+__device__ __forceinline__ void copy_async16(void* smem, const void* src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(src),
+                 "r"(real ? 16 : 0) : "memory");   // what is not there is filled with zeros
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Rows of one tensor, fetched tile by tile: each thread reads back what it copied itself.
-template <typename E, int VEC, int N, int THREADS, bool STAGED> struct Fetch {
-    Raw<E, VEC> r[N];
-    __device__ __forceinline__ static void ask(char* stage, const E* p, size_t pitch, int live)
+// A warp's TPG rows of one tensor.  Staged: the warp copies them in 16-byte pieces to its own part of shared memory.
+template <typename E, typename V> struct Fetch {
+    Raw<E, V::VEC> r[V::TPG];
+    static constexpr int ROW = V::CB * (int)sizeof(E), BYTES = V::TPG * ROW;   // of a warp
+    // p: the block's first channel of the warp's first row; cols: channels of the block that there are
+    __device__ __forceinline__ static void ask(char* part, const E* p, size_t pitch, int live, int cols)
     {
-        if constexpr (STAGED) {
+        if constexpr (V::STAGED) {
+            constexpr int PIECES = ROW / 16, ROWS = 32 / PIECES, PER = 16 / (int)sizeof(E);
+            const int lane = threadIdx.x & 31, row = lane / PIECES, col = (lane % PIECES) * PER;
+            const bool in = col < cols;
+            const E* from = p + (in ? row * pitch + col : 0);
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                copy_async<VEC * (int)sizeof(E)>(stage + (size_t)(i * THREADS + threadIdx.x) * VEC * sizeof(E),
-                                                 i < live ? p + i * pitch : p, i < live);
+            for (int i = 0; i < V::TPG; i += ROWS) {
+                const bool real = in && i + row < live;
+                copy_async16(part + i * ROW + lane * 16, real ? from + i * pitch : p, real);
+            }
         }
     }
-    __device__ __forceinline__ void take(const char* stage, const E* p, size_t pitch, int live)
+    __device__ __forceinline__ void take(const char* part, const E* p, size_t pitch, int live, int col, bool in)
     {
+        const int lane = threadIdx.x & 31;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (STAGED) {
-                r[i] = *reinterpret_cast<const Raw<E, VEC>*>(stage + (size_t)(i * THREADS + threadIdx.x) * VEC * sizeof(E));
+        for (int i = 0; i < V::TPG; ++i) {
+            if constexpr (V::STAGED) {
+                r[i] = *reinterpret_cast<const Raw<E, V::VEC>*>(part + i * ROW + lane * V::VEC * sizeof(E));
             } else {
-                r[i] = Raw<E, VEC>{};
-                if (i < live) r[i] = *reinterpret_cast<const Raw<E, VEC>*>(p + i * pitch);
+                r[i] = Raw<E, V::VEC>{};
+                if (in && i < live) r[i] = *reinterpret_cast<const Raw<E, V::VEC>*>(p + i * pitch + col);
             }
         }
     }
 };
 
-// Where sequences begin and end among a group's rows t .. t+n-1 (bit i: row t + i); s: the sequence of row t.
+// Where sequences begin and end among a warp's rows t .. t+n-1 (bit i: row t + i); s: the sequence of row t.  The sequence of
+// the last search is kept: a warp whose rows lie inside it reads nothing.
 struct Marks {
     unsigned first = 0, last = 0;
     int s = 0;
+    int begin = 0, end = 0;   // of the sequence last searched for
     __device__ __forceinline__ void find(const ScanArgs& a, int t, int n, int limit)
     {
         first = last = 0;
         if (t >= limit) return;
         n = min(n, limit - t);
-        s = a.cu ? seq_of({a.cu, a.S, a.rows}, t) : t / a.T;
-        for (int q = s, at = a.begin(q) == t ? t : -1;;) {
-            if (at >= 0) first |= 1u << (at - t);
-            const int end = max(a.begin(q + 1), max(at, t) + 1);
-            if (end > t + n) break;
-            last |= 1u << (end - 1 - t);
-            if (end >= t + n) break;
-            q = next(a, q, end);
-            at = end;
+        if (t > begin && t + n < end) return;
+        if (!a.cu) {
+            s = t / a.T;
+            begin = s * a.T;
+            end = begin + a.T;
+            for (int at = begin; at < t + n; at += a.T) {
+                if (at >= t) first |= 1u << (at - t);
+                if (at + a.T <= t + n) last |= 1u << (at + a.T - 1 - t);
+            }
+            return;
+        }
+        // the last sequence that begins at or before t: 32 probes at a time
+        const int lane = threadIdx.x & 31;
+        int lo = 0, hi = a.S;
+        while (hi - lo > 1) {
+            const int pitch = (hi - lo + 31) / 32, i = lo + lane * pitch;
+            const unsigned before = __ballot_sync(~0u, i < hi && a.cu[i] <= t);
+            lo += (max(__popc(before), 1) - 1) * pitch;
+            hi = min(hi, lo + pitch);
+        }
+        s = lo;
+        begin = a.cu[s];
+        end = a.cu[s + 1];
+        for (int q = s; q < a.S; q += 32) {
+            const bool in = q + lane < a.S;
+            const int b = in ? a.cu[q + lane] : 0, e = in ? a.cu[q + lane + 1] : 0;
+            const bool f = e > b && b >= t && b < t + n, l = e > b && e > t && e <= t + n;
+            first |= __reduce_or_sync(~0u, f ? 1u << (b - t) : 0u);
+            last |= __reduce_or_sync(~0u, l ? 1u << (e - 1 - t) : 0u);
+            if (__shfl_sync(~0u, in && e < t + n, 31) == 0) break;
         }
     }
     // the sequence that row t belongs to, the one before it being of sequence q
@@ -150,26 +262,21 @@ __device__ __forceinline__ uint32_t cluster_rank()
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_meet()
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+template <int N> __device__ __forceinline__ F<N> read_remote(const float* mine, uint32_t rank)
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    uint32_t at;
+    F<N> a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+    if constexpr (N == 2) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(a.x[0]), "=f"(a.x[1]) : "r"(at) : "memory");
+    else asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(a.x[0]) : "r"(at) : "memory");
+    return a;
 }
-template <int VEC> __device__ __forceinline__ void store_remote(float* mine, uint32_t rank, const float (&x)[VEC])
-{
-    uint32_t to;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
-    if constexpr (VEC == 4)
-        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]) : "memory");
-    else
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(x[0]) : "memory");
-}
+// One warp announces, another one waits: named barriers of 64 threads.
+__device__ __forceinline__ void hand_on(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void take_over(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
-// A stretch of rows maps the state in front of it to a h + b: the sum of its log gates, and b.
-template <int VEC> struct Affine {
-    float g[VEC], b[VEC];
-};
-
-__device__ __forceinline__ int div_up_dev(int a, int b) { return (a + b - 1) / b; }
 // The sequence in front of q that is not empty (one there is: q does not begin the rows).
 __device__ __forceinline__ int previous(const ScanArgs& a, int q)
 {
@@ -179,408 +286,360 @@ __device__ __forceinline__ int previous(const ScanArgs& a, int q)
     return max(q, 0);
 }
 
-// What the warps of a CTA (and the CTAs of a walk) tell one another: factor and b of their stretch; two sets, used in turn.
-template <typename V> struct Exchange {
-    float v[2][V::WARPS][V::CB], b[2][V::WARPS][V::CB], g[2][V::WARPS][V::CB];
-    float cv[2][MAX_SPAN][V::CB], cb[2][MAX_SPAN][V::CB];
-    // shared memory that a walk of `span` CTAs needs of it: a single one has no use for the last two
-    static size_t bytes(int span) { return span > 1 ? sizeof(Exchange) : offsetof(Exchange, cv); }
-};
-template <typename V> struct Inner {   // the same for maps that stay inside a CTA
-    float v[2][V::WARPS][V::CB], b[2][V::WARPS][V::CB];
+template <typename V> struct Hand {
+    float state[V::WARPS][V::CB];                    // in front of the unit that warp w takes next
+    float g[V::WARPS][V::CB], b[V::WARPS][V::CB];    // a split walk: the maps of the warps' stretches, then [0] the CTA's
 };
 
-// Within a warp, in the order of time (REVERSE: against it): `m` becomes the map of the stretches in front of this thread's own,
-// and the warp's whole map goes to the exchange.
-template <typename V, bool REVERSE, bool TOTALS, typename X>
-__device__ __forceinline__ void meet_warp(Affine<V::VEC>& m, X& ex, int set)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, place = lane / V::LANES, c = (lane % V::LANES) * V::VEC;
-#pragma unroll
-    for (int d = 1; d < V::PER_WARP; d <<= 1) {
-        const bool in = REVERSE ? place + d < V::PER_WARP : place >= d;
-#pragma unroll
-        for (int k = 0; k < V::VEC; ++k) {
-            const float g = REVERSE ? __shfl_down_sync(~0u, m.g[k], d * V::LANES) : __shfl_up_sync(~0u, m.g[k], d * V::LANES);
-            const float b = REVERSE ? __shfl_down_sync(~0u, m.b[k], d * V::LANES) : __shfl_up_sync(~0u, m.b[k], d * V::LANES);
-            if (in) {
-                m.b[k] = Decay::of(m.g[k]).step(b, m.b[k]);
-                m.g[k] += g;
-            }
-        }
-    }
-    if (place == (REVERSE ? 0 : V::PER_WARP - 1)) {
-        float v[V::VEC];
-#pragma unroll
-        for (int k = 0; k < V::VEC; ++k) v[k] = Decay::of(m.g[k]).v;
-        store_vec<V::VEC>(&ex.v[set][warp][c], v);
-        store_vec<V::VEC>(&ex.b[set][warp][c], m.b);
-        if constexpr (TOTALS) store_vec<V::VEC>(&ex.g[set][warp][c], m.g);
-    }
-#pragma unroll
-    for (int k = 0; k < V::VEC; ++k) {
-        if constexpr (V::PER_WARP > 1) {
-            const float g = REVERSE ? __shfl_down_sync(~0u, m.g[k], V::LANES) : __shfl_up_sync(~0u, m.g[k], V::LANES);
-            const float b = REVERSE ? __shfl_down_sync(~0u, m.b[k], V::LANES) : __shfl_up_sync(~0u, m.b[k], V::LANES);
-            const bool in = REVERSE ? place + 1 < V::PER_WARP : place > 0;
-            m.g[k] = in ? g : 0.f;
-            m.b[k] = in ? b : 0.f;
-        } else {
-            m.g[k] = 0.f;
-            m.b[k] = 0.f;
-        }
-    }
-}
-
-template <int VEC> __device__ __forceinline__ void advance(float (&h)[VEC], const float* v, const float* b)
-{
-    float x[VEC], y[VEC];
-    load_vec<VEC>(v, x);
-    load_vec<VEC>(b, y);
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) h[k] = Decay{x[k]}.step(h[k], y[k]);
-}
-
-// The CTA's whole map to every CTA of the walk (warp w to ranks w, w + WARPS, ..), behind a barrier that follows meet_warp.
-template <typename V, bool REVERSE> __device__ __forceinline__ void tell_walk(Exchange<V>& ex, int set, uint32_t rank, int span)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane * V::VEC;
-    if (lane >= V::LANES || warp >= span) return;
-    float g[V::VEC] = {}, b[V::VEC] = {}, v[V::VEC];
-    for (int j = 0; j < V::WARPS; ++j) {
-        const int w = REVERSE ? V::WARPS - 1 - j : j;
-        float x[V::VEC];
-        load_vec<V::VEC>(&ex.g[set][w][c], x);
-        advance<V::VEC>(b, &ex.v[set][w][c], &ex.b[set][w][c]);
-#pragma unroll
-        for (int k = 0; k < V::VEC; ++k) g[k] += x[k];
-    }
-#pragma unroll
-    for (int k = 0; k < V::VEC; ++k) v[k] = Decay::of(g[k]).v;
-    for (int r = warp; r < span; r += V::WARPS) {
-        store_remote<V::VEC>(&ex.cv[set][rank][c], r, v);
-        store_remote<V::VEC>(&ex.cb[set][rank][c], r, b);
-    }
-}
-
-// The walk's state `base` through this tile row of CTAs; `mine`: in front of this CTA, then of this warp.
-template <typename V, bool REVERSE>
-__device__ __forceinline__ void fold(float (&base)[V::VEC], float (&mine)[V::VEC], float (&front)[V::VEC], const Exchange<V>& ex,
-                                     int set, uint32_t rank, int span)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = (lane % V::LANES) * V::VEC;
-    if (span > 1) {
-        for (int r = 0; r < span; ++r) {
-            if (r == (int)rank)
-#pragma unroll
-                for (int k = 0; k < V::VEC; ++k) mine[k] = base[k];
-            advance<V::VEC>(base, &ex.cv[set][r][c], &ex.cb[set][r][c]);
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < V::VEC; ++k) mine[k] = base[k];
-    }
-#pragma unroll
-    for (int k = 0; k < V::VEC; ++k) front[k] = mine[k];
-    for (int j = 0; j < V::WARPS; ++j) {
-        const int w = REVERSE ? V::WARPS - 1 - j : j;
-        if (w == warp) {
-#pragma unroll
-            for (int k = 0; k < V::VEC; ++k) mine[k] = front[k];
-            if (span > 1) break;
-        }
-        advance<V::VEC>(front, &ex.v[set][w][c], &ex.b[set][w][c]);
-    }
-    if (span == 1) {
-#pragma unroll
-        for (int k = 0; k < V::VEC; ++k) base[k] = front[k];
-    }
-}
-
-// A state of an empty sequence (or its gradient) passes through; `place` of `places` thread groups of the walk.
-template <int VEC>
+// A state of an empty sequence (or its gradient) passes through; `place` of `places` warps of the walk.
+template <int N>
 __device__ __forceinline__ void pass_empty(const ScanArgs& a, const float* from, float* to, int place, int places, int c)
 {
-    for (int s = place; s < a.S; s += places) {
-        if (a.cu[s + 1] > a.cu[s]) continue;
-        float v[VEC] = {};
-        if (from) load_vec<VEC>(from + (size_t)s * a.C + c, v);
-        store_vec<VEC>(to + (size_t)s * a.C + c, v);
-    }
+    for (int s = place; s < a.S; s += places)
+        if (a.cu[s + 1] <= a.cu[s]) write<N>(to + (size_t)s * a.C + c, read_or_zero<N>(from, (size_t)s * a.C + c));
 }
 
-// One walk = one dense sequence, or a whole flat batch with resets where sequences begin, over CB channels.  The walk's CTAs
-// (span of them, one cluster) take a row of tiles at a time, each TILE rows: every thread maps its TPG rows to (sum of gates,
-// b), the maps are combined over warp, CTA and cluster, and the rows are walked a second time from registers with the state
-// in front of them.  out == nullptr: only the states are kept.
-template <typename V, bool COMP, bool FLAT>
-__global__ void __launch_bounds__(V::THREADS, 512 / V::THREADS) scan_fwd_kernel(ScanArgs a)
+// Where a CTA stands: its walk, its channels, and the rows that there are.
+template <typename V, bool FLAT, bool SPLIT> struct Stand {
+    int rank, s, c0, c, warp, limit, first, last;   // units first .. last-1 of the walk are this CTA's
+    bool inside, whole;                             // this lane's channels are there; all of the block's are
+    size_t row0;                                    // the walk's first row
+    __device__ __forceinline__ Stand(const ScanArgs& a)
+    {
+        rank = SPLIT ? (int)cluster_rank() : 0;
+        const int nblk = (a.C + V::CB - 1) / V::CB, walk = SPLIT ? blockIdx.x / a.span : blockIdx.x;
+        s = walk / nblk;
+        c0 = (walk % nblk) * V::CB;
+        c = c0 + (threadIdx.x & 31) * V::VEC;
+        warp = threadIdx.x >> 5;
+        inside = c < a.C;
+        whole = c0 + V::CB <= a.C;
+        limit = FLAT && a.cu ? min(max(a.cu[a.S], 0), a.rows) : a.rows;
+        row0 = FLAT ? 0 : (size_t)s * a.rows;
+        const int per = SPLIT ? (a.units + a.span - 1) / a.span : a.units;
+        first = min(rank * per, a.units);
+        last = min(first + per, a.units);
+    }
+    __device__ __forceinline__ int live(int t) const { return min(max(limit - t, 0), UNIT); }
+};
+
+// A split walk's first pass over the CTA's rows: what they do to the state in front of them, as (sum of gates, b), and from
+// the other CTAs' the state in front of this one.  REVERSE: for e = a (y + e), from the end.  Warp 0 has the result.
+template <typename V, bool COMP, bool FLAT, bool REVERSE, typename S>
+__device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& at, Hand<V>& hand, F<V::VEC> h, const float* gate,
+                                                    const typename V::T* x, char* gpart, char* xpart)
 {
-    using T = typename V::T;
-    extern __shared__ __align__(16) char shared[];
-    Exchange<V>& ex = *reinterpret_cast<Exchange<V>*>(shared + V::STAGED * TILE * V::CB * (4 + sizeof(T)));
-    char* const stage = shared;
-    pdl_wait();
-    constexpr int VEC = V::VEC, TPG = V::TPG;
-    const int lane = threadIdx.x & 31, group = threadIdx.x / V::LANES;
-    const uint32_t rank = a.span > 1 ? cluster_rank() : 0;
-    const int nblk = div_up_dev(a.C, V::CB);
-    const int walk = blockIdx.x / a.span, s = walk / nblk;
-    const int c = (walk % nblk) * V::CB + (lane % V::LANES) * VEC;
-    const bool inside = c < a.C;
-    const int limit = FLAT ? (a.cu ? min(max(a.cu[a.S], 0), a.rows) : a.rows) : a.rows;
-    const size_t row0 = FLAT ? 0 : (size_t)s * a.rows;
-    const T* x = static_cast<const T*>(a.x) + row0 * a.C + c;
-    const float* gate = a.gate + row0 * a.C + c;
-    T* out = static_cast<T*>(a.out) + row0 * a.C + c;
-    float* saved = a.saved ? a.saved + (FLAT ? 0 : (size_t)s * a.tiles * a.C) + c : nullptr;
-    if (FLAT && a.cu && a.fin && inside)
-        pass_empty<VEC>(a, a.init, a.fin, rank * (V::THREADS / V::LANES) + group, a.span * (V::THREADS / V::LANES), c);
-    float base[VEC] = {};
-    if (!FLAT && a.init && inside) load_vec<VEC>(a.init + (size_t)s * a.C + c, base);
-    char* gstage = stage;
-    char* xstage = stage + V::THREADS * TPG * VEC * 4;
-    const int steps = div_up_dev(a.tiles, a.span);
-    using FetchG = Fetch<float, VEC, TPG, V::THREADS, V::STAGED>;
-    using FetchX = Fetch<T, VEC, TPG, V::THREADS, V::STAGED>;
-    auto row_of = [&](int step) { return (step * a.span + (int)rank) * TILE + group * TPG; };
-    auto live_of = [&](int t) { return inside ? min(max(limit - t, 0), TPG) : 0; };
-    auto ask = [&](int step) {
-        const int t = row_of(step), live = live_of(t);
-        const size_t at = live ? (size_t)t * a.C : 0;
-        FetchG::ask(gstage, inside ? gate + at : a.gate, a.C, live);
-        FetchX::ask(xstage, inside ? x + at : static_cast<const T*>(a.x), a.C, live);
+    using FetchG = Fetch<float, V>;
+    using FetchX = Fetch<typename V::T, V>;
+    constexpr int N = V::VEC;
+    const int l = (threadIdx.x & 31) * N, per = (at.last - at.first + V::WARPS - 1) / V::WARPS;
+    const int lo = min(at.first + at.warp * per, at.last), hi = min(lo + per, at.last);
+    auto unit = [&](int i) { return REVERSE ? hi - 1 - i : lo + i; };
+    auto ask = [&](int i) {
+        const int t = unit(i) * UNIT, live = at.live(t);
+        const size_t row = live ? (size_t)t * a.C : 0;
+        FetchG::ask(gpart, gate + row, a.C, live, a.C - at.c0);
+        FetchX::ask(xpart, x + row, a.C, live, a.C - at.c0);
     };
-    if (V::STAGED) ask(0);
-    if (a.span > 1) cluster_meet();   // every CTA of the walk runs before another one writes to its shared memory
-    for (int step = 0; step < steps; ++step) {
-        const int t = row_of(step), live = live_of(t), set = step & 1;
-        const size_t at = (size_t)t * a.C;
-        Marks marks;
-        if (FLAT) marks.find(a, t, TPG, limit);
+    F<N> mg = all<N>(0.f), mb = mg;
+    Marks marks;
+    if (V::STAGED && lo < hi) ask(0);
+    for (int i = 0; i < hi - lo; ++i) {
+        const int t = unit(i) * UNIT, live = at.live(t);
+        const size_t row = live ? (size_t)t * a.C : 0;
+        if (FLAT) marks.find(a, t, UNIT, at.limit);
         FetchG fg;
         FetchX fx;
-        if (V::STAGED) copies_wait();
-        fg.take(gstage, gate + at, a.C, live);
-        fx.take(xstage, x + at, a.C, live);
-        Decay d[TPG][VEC];
-        Affine<VEC> m = {};
+        if (V::STAGED) {
+            copies_wait();
+            __syncwarp();
+        }
+        fg.take(gpart, gate + row, a.C, live, at.c - at.c0, at.inside);
+        fx.take(xpart, x + row, a.C, live, at.c - at.c0, at.inside);
+        __syncwarp();
+        if (V::STAGED && i + 1 < hi - lo) ask(i + 1);
         int q = marks.s;
+        if (FLAT && REVERSE)
+            for (int k = 1; k < UNIT; ++k)
+                if (marks.first >> k & 1) q = Marks::next(a, q, t + k);
 #pragma unroll
-        for (int i = 0; i < TPG; ++i) {
-            if (FLAT && (marks.first >> i & 1)) {
-                if (i) q = Marks::next(a, q, t + i);
-                float h[VEC] = {};
-                if (a.init && inside) load_vec<VEC>(a.init + (size_t)q * a.C + c, h);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) { m.b[k] = h[k]; m.g[k] = -INFINITY; }
+        for (int k = 0; k < UNIT; ++k) {
+            const int j = REVERSE ? UNIT - 1 - k : k;
+            const F<N> g = fg.r[j].get(), y = fx.r[j].get();
+            const Decay<N> d = Decay<N>::of(g);
+            if (FLAT && !REVERSE && (marks.first >> j & 1)) {
+                if (j) q = Marks::next(a, q, t + j);
+                mb = at.inside ? read_or_zero<N>(a.init, (size_t)q * a.C + at.c) : all<N>(0.f);
+                mg = all<N>(-INFINITY);
             }
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float g = fg.r[i].get(k);
-                d[i][k] = Decay::of(g);
-                const float y = fx.r[i].get(k);
-                m.g[k] += g;
-                m.b[k] = d[i][k].step(m.b[k], COMP ? d[i][k].complement() * y : y);
+            if (FLAT && REVERSE && (marks.last >> j & 1)) {
+                mb = at.inside ? read_or_zero<N>(a.dfin, (size_t)q * a.C + at.c) : all<N>(0.f);
+                mg = all<N>(-INFINITY);
             }
-        }
-        meet_warp<V, false, true>(m, ex, set);
-        __syncthreads();
-        if (V::STAGED && step + 1 < steps) ask(step + 1);
-        if (a.span > 1) {
-            tell_walk<V, false>(ex, set, rank, a.span);
-            cluster_meet();
-        }
-        float h[VEC], front[VEC];
-        float mine[VEC];
-        fold<V, false>(base, mine, front, ex, set, rank, a.span);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) h[k] = Decay::of(m.g[k]).step(mine[k], m.b[k]);
-        if (saved && group == 0 && inside && t < a.tiles * TILE) store_vec<VEC>(saved + (size_t)(t / TILE) * a.C, h);
-        q = marks.s;
-#pragma unroll
-        for (int i = 0; i < TPG; ++i) {
-            if (i >= live) break;
-            if (FLAT && (marks.first >> i & 1)) {
-                if (i) q = Marks::next(a, q, t + i);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) h[k] = 0.f;
-                if (a.init) load_vec<VEC>(a.init + (size_t)q * a.C + c, h);
-            }
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float y = fx.r[i].get(k);
-                h[k] = d[i][k].step(h[k], COMP ? d[i][k].complement() * y : y);
-            }
-            if (a.out) store_vec<VEC>(out + at + (size_t)i * a.C, h);
-            if (FLAT && a.fin && (marks.last >> i & 1)) store_vec<VEC>(a.fin + (size_t)q * a.C + c, h);
+            mg = add(mg, g);
+            mb = REVERSE ? d.times(add(y, mb)) : d.step(mb, COMP ? mul(d.complement(), y) : y);
+            if (FLAT && REVERSE && j && (marks.first >> j & 1)) q = previous(a, q);
         }
     }
-    if (!FLAT && a.fin && inside && rank == 0 && group == 0) store_vec<VEC>(a.fin + (size_t)s * a.C + c, base);
+    write<N>(&hand.g[at.warp][l], mg);
+    write<N>(&hand.b[at.warp][l], mb);
+    __syncthreads();
+    if (at.warp == 0) {
+        F<N> g = all<N>(0.f), b = g;
+#pragma unroll
+        for (int k = 0; k < V::WARPS; ++k) {
+            const int w = REVERSE ? V::WARPS - 1 - k : k;
+            const F<N> wg = read<N>(&hand.g[w][l]);
+            b = Decay<N>::of(wg).step(b, read<N>(&hand.b[w][l]));
+            g = add(g, wg);
+        }
+        write<N>(&hand.g[0][l], g);
+        write<N>(&hand.b[0][l], b);
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (at.warp == 0)
+        for (int r = REVERSE ? a.span - 1 : 0; r != at.rank; r += REVERSE ? -1 : 1)
+            h = Decay<N>::of(read_remote<N>(&hand.g[0][l], r)).step(h, read_remote<N>(&hand.b[0][l], r));
+    cluster_arrive();   // nobody leaves, or writes there again, before all have read: waited for at the end
+    return h;
 }
 
-// The same walk from the end: e = a (dout + e), the state's gradient as the row before sees it.  Each tile walks its states
-// forward again from the one that the forward kept, so that the gates' gradients take fp32 states:
-//   dgate_t = (h_{t-1} [- x_t]) e_t,   dx_t = dh_t or (1 - a_t) dh_t,   dh_t = dout_t + e_{t+1}.
-template <typename V, bool COMP, bool FLAT>
-__global__ void __launch_bounds__(V::THREADS, 512 / V::THREADS) scan_bwd_kernel(ScanArgs a)
+// One walk = one dense sequence, or a whole flat batch with resets where sequences begin, over CB channels.  A CTA's warps take
+// units of UNIT rows in turn: a warp maps its rows to (sum of gates, b), waits for the state in front of them, hands the
+// state behind them on to the next warp before it does anything else, and walks the rows a second time from registers.  So
+// the only thing done one after another is a step of two fmas a unit (about 100 cycles from warp to warp by named barriers);
+// with barriers of all warps instead, tile by tile, the warps waited more than they worked (38 to 51 us against XX).
+// Few walks are split among the CTAs of a cluster, which read their rows once more for the state in front of them.
+// Rows that are all there and begin and end no sequence take the code without tests.
+// out == nullptr: only the states are kept.
+template <typename V, bool COMP, bool FLAT, bool SPLIT>
+__global__ void __launch_bounds__(32 * V::WARPS, XFMIN / V::WARPS) scan_fwd_kernel(ScanArgs a)
 {
     using T = typename V::T;
+    using FetchG = Fetch<float, V>;
+    using FetchX = Fetch<T, V>;
+    constexpr int N = V::VEC;
     extern __shared__ __align__(16) char shared[];
-    Inner<V>& inner = *reinterpret_cast<Inner<V>*>(shared);
-    char* const stage = shared + sizeof(Inner<V>);
-    Exchange<V>& ex = *reinterpret_cast<Exchange<V>*>(stage + V::STAGED * TILE * V::CB * (4 + 2 * sizeof(T)));
     pdl_wait();
-    constexpr int VEC = V::VEC, TPG = V::TPG;
-    const int lane = threadIdx.x & 31, group = threadIdx.x / V::LANES;
-    const uint32_t rank = a.span > 1 ? cluster_rank() : 0;
-    const int nblk = div_up_dev(a.C, V::CB);
-    const int walk = blockIdx.x / a.span, s = walk / nblk;
-    const int c = (walk % nblk) * V::CB + (lane % V::LANES) * VEC;
-    const bool inside = c < a.C;
-    const int limit = FLAT ? (a.cu ? min(max(a.cu[a.S], 0), a.rows) : a.rows) : a.rows;
-    const size_t row0 = FLAT ? 0 : (size_t)s * a.rows;
-    const T* x = static_cast<const T*>(a.x) + row0 * a.C + c;
-    const T* dout = static_cast<const T*>(a.dout) + row0 * a.C + c;
-    const float* gate = a.gate + row0 * a.C + c;
-    T* dx = static_cast<T*>(a.dx) + row0 * a.C + c;
-    float* dgate = a.dgate + row0 * a.C + c;
-    const float* saved = a.saved + (FLAT ? 0 : (size_t)s * a.tiles * a.C) + c;
-    if (FLAT && a.cu && a.dinit && inside)
-        pass_empty<VEC>(a, a.dfin, a.dinit, rank * (V::THREADS / V::LANES) + group, a.span * (V::THREADS / V::LANES), c);
-    float base[VEC] = {};
-    if (!FLAT && a.dfin && inside) load_vec<VEC>(a.dfin + (size_t)s * a.C + c, base);
-    char* gstage = stage;
-    char* xstage = gstage + V::THREADS * TPG * VEC * 4;
-    char* ystage = xstage + V::THREADS * TPG * VEC * sizeof(T);
-    const int steps = div_up_dev(a.tiles, a.span);
-    using FetchG = Fetch<float, VEC, TPG, V::THREADS, V::STAGED>;
-    using FetchX = Fetch<T, VEC, TPG, V::THREADS, V::STAGED>;
-    auto row_of = [&](int step) { return (a.tiles - 1 - step * a.span - (int)rank) * TILE + group * TPG; };   // < 0: none
-    auto live_of = [&](int t) { return inside && t >= 0 ? min(max(limit - t, 0), TPG) : 0; };
-    auto ask = [&](int step) {
-        const int t = row_of(step), live = live_of(t);
-        const size_t at = live ? (size_t)t * a.C : 0;
-        FetchG::ask(gstage, inside ? gate + at : a.gate, a.C, live);
-        FetchX::ask(xstage, inside ? x + at : static_cast<const T*>(a.x), a.C, live);
-        FetchX::ask(ystage, inside ? dout + at : static_cast<const T*>(a.dout), a.C, live);
+    const Stand<V, FLAT, SPLIT> at(a);
+    Hand<V>& hand = *reinterpret_cast<Hand<V>*>(shared);
+    char* const gpart = shared + sizeof(Hand<V>) + at.warp * (FetchG::BYTES + FetchX::BYTES);
+    char* const xpart = gpart + FetchG::BYTES;
+    const int c = at.c, l = (threadIdx.x & 31) * N;
+    const T* x = static_cast<const T*>(a.x) + at.row0 * a.C + at.c0;
+    const float* gate = a.gate + at.row0 * a.C + at.c0;
+    T* out = static_cast<T*>(a.out) + at.row0 * a.C + c;
+    float* saved = a.saved ? a.saved + (FLAT ? 0 : (size_t)at.s * a.units * a.C) + c : nullptr;
+    if (FLAT && a.cu && a.fin && at.inside) pass_empty<N>(a, a.init, a.fin, at.rank * V::WARPS + at.warp, a.span * V::WARPS, c);
+    F<N> h = all<N>(0.f);
+    if (!FLAT && at.inside) h = read_or_zero<N>(a.init, (size_t)at.s * a.C + c);
+    if (SPLIT) h = state_in_front<V, COMP, FLAT, false>(a, at, hand, h, gate, x, gpart, xpart);
+    auto ask = [&](int u) {
+        const int t = u * UNIT, live = at.live(t);
+        const size_t row = live ? (size_t)t * a.C : 0;
+        FetchG::ask(gpart, gate + row, a.C, live, a.C - at.c0);
+        FetchX::ask(xpart, x + row, a.C, live, a.C - at.c0);
     };
-    if (V::STAGED) ask(0);
-    if (a.span > 1) cluster_meet();   // every CTA of the walk runs before another one writes to its shared memory
-    for (int step = 0; step < steps; ++step) {
-        const int t = row_of(step), live = live_of(t), set = step & 1;
-        const size_t at = t >= 0 ? (size_t)t * a.C : 0;
-        Marks marks;
-        if (FLAT && t >= 0) marks.find(a, t, TPG, limit);
+    Marks marks;
+    int u = at.first + at.warp;
+    if (V::STAGED && u < at.last) ask(u);
+    for (; u < at.last; u += V::WARPS) {
+        const int t = u * UNIT, live = at.live(t);
+        const size_t row = (size_t)t * a.C;
+        if (FLAT) marks.find(a, t, UNIT, at.limit);
+        const bool plain = live == UNIT && at.whole && !(FLAT && (marks.first | marks.last));
+        FetchG fg;
+        FetchX fx;
+        if (V::STAGED) {
+            copies_wait();
+            __syncwarp();
+        }
+        fg.take(gpart, gate + row, a.C, live, c - at.c0, at.inside);
+        fx.take(xpart, x + row, a.C, live, c - at.c0, at.inside);
+        __syncwarp();
+        if (V::STAGED && u + V::WARPS < at.last) ask(u + V::WARPS);
+        Decay<N> d[UNIT];
+        F<N> b[UNIT];
+        F<N> mg = all<N>(0.f), mb = mg;
+#pragma unroll
+        for (int i = 0; i < UNIT; ++i) {
+            const F<N> g = fg.r[i].get(), y = fx.r[i].get();
+            d[i] = Decay<N>::of(g);
+            b[i] = COMP ? mul(d[i].complement(), y) : y;
+            mg = add(mg, g);
+            mb = d[i].step(mb, b[i]);
+        }
+        if (FLAT && marks.first) {
+            int q = marks.s;
+#pragma unroll
+            for (int i = 0; i < UNIT; ++i) {
+                if (marks.first >> i & 1) {
+                    if (i) q = Marks::next(a, q, t + i);
+                    mb = at.inside ? read_or_zero<N>(a.init, (size_t)q * a.C + c) : all<N>(0.f);
+                }
+                mb = d[i].step(mb, b[i]);
+            }
+            mg = all<N>(-INFINITY);
+        }
+        const Decay<N> md = Decay<N>::of(mg);
+        if (u > at.first) {
+            take_over(at.warp);
+            h = read<N>(&hand.state[at.warp][l]);
+        }
+        const F<N> behind = md.step(h, mb);
+        if (u + 1 < at.last) {
+            const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
+            write<N>(&hand.state[next][l], behind);
+            hand_on(next);
+        }
+        if (!FLAT && a.fin && u + 1 == a.units && at.inside) write<N>(a.fin + (size_t)at.s * a.C + c, behind);
+        if (plain) {
+            if (saved) write<N>(saved + (size_t)u * a.C, h);
+#pragma unroll
+            for (int i = 0; i < UNIT; ++i) {
+                h = d[i].step(h, b[i]);
+                if (a.out) write<N>(out + row + (size_t)i * a.C, h);
+            }
+        } else if (at.inside) {
+            if (saved) write<N>(saved + (size_t)u * a.C, h);
+            int q = marks.s;
+#pragma unroll
+            for (int i = 0; i < UNIT; ++i) {
+                if (i >= live) break;
+                if (FLAT && (marks.first >> i & 1)) {
+                    if (i) q = Marks::next(a, q, t + i);
+                    h = read_or_zero<N>(a.init, (size_t)q * a.C + c);
+                }
+                h = d[i].step(h, b[i]);
+                if (a.out) write<N>(out + row + (size_t)i * a.C, h);
+                if (FLAT && a.fin && (marks.last >> i & 1)) write<N>(a.fin + (size_t)q * a.C + c, h);
+            }
+        }
+    }
+    if (SPLIT) cluster_wait();
+}
+
+// The same walk from the end: e = a (dout + e), the state's gradient as the row before sees it.  Each unit walks its states
+// forward again from the one that the forward kept, so that the gates' gradients take fp32 states:
+//   dgate_t = (h_{t-1} [- x_t]) e_t,   dx_t = dh_t or (1 - a_t) dh_t,   dh_t = dout_t + e_{t+1}.
+template <typename V, bool COMP, bool FLAT, bool SPLIT>
+__global__ void __launch_bounds__(32 * V::WARPS, XBMIN / V::WARPS) scan_bwd_kernel(ScanArgs a)
+{
+    using T = typename V::T;
+    using FetchG = Fetch<float, V>;
+    using FetchX = Fetch<T, V>;
+    constexpr int N = V::VEC, PART = FetchG::BYTES + 2 * FetchX::BYTES;
+    extern __shared__ __align__(16) char shared[];
+    pdl_wait();
+    const Stand<V, FLAT, SPLIT> at(a);
+    Hand<V>& hand = *reinterpret_cast<Hand<V>*>(shared);
+    char* const gpart = shared + sizeof(Hand<V>) + at.warp * PART;
+    char* const xpart = gpart + FetchG::BYTES;
+    char* const ypart = xpart + FetchX::BYTES;
+    const int c = at.c, l = (threadIdx.x & 31) * N;
+    const T* x = static_cast<const T*>(a.x) + at.row0 * a.C + at.c0;
+    const T* dout = static_cast<const T*>(a.dout) + at.row0 * a.C + at.c0;
+    const float* gate = a.gate + at.row0 * a.C + at.c0;
+    T* dx = static_cast<T*>(a.dx) + at.row0 * a.C + c;
+    float* dgate = a.dgate + at.row0 * a.C + c;
+    const float* saved = a.saved + (FLAT ? 0 : (size_t)at.s * a.units * a.C) + c;
+    if (FLAT && a.cu && a.dinit && at.inside) pass_empty<N>(a, a.dfin, a.dinit, at.rank * V::WARPS + at.warp, a.span * V::WARPS, c);
+    F<N> e = all<N>(0.f);
+    if (!FLAT && at.inside) e = read_or_zero<N>(a.dfin, (size_t)at.s * a.C + c);
+    if (SPLIT) e = state_in_front<V, COMP, FLAT, true>(a, at, hand, e, gate, dout, gpart, ypart);
+    auto ask = [&](int u) {
+        const int t = u * UNIT, live = at.live(t);
+        const size_t row = live ? (size_t)t * a.C : 0;
+        FetchG::ask(gpart, gate + row, a.C, live, a.C - at.c0);
+        FetchX::ask(xpart, x + row, a.C, live, a.C - at.c0);
+        FetchX::ask(ypart, dout + row, a.C, live, a.C - at.c0);
+    };
+    Marks marks;
+    int u = at.last - 1 - at.warp;
+    if (V::STAGED && u >= at.first) ask(u);
+    for (; u >= at.first; u -= V::WARPS) {
+        const int t = u * UNIT, live = at.live(t);
+        const size_t row = (size_t)t * a.C;
+        if (FLAT) marks.find(a, t, UNIT, at.limit);
+        const bool plain = live == UNIT && at.whole && !(FLAT && (marks.first | marks.last));
+        F<N> h = all<N>(0.f);
+        if (at.inside) h = read<N>(saved + (size_t)u * a.C);
         FetchG fg;
         FetchX fx, fy;
-        float h[VEC] = {};
-        if (live) load_vec<VEC>(saved + (size_t)(t / TILE) * a.C, h);
-        if (V::STAGED) copies_wait();
-        fg.take(gstage, gate + at, a.C, live);
-        fx.take(xstage, x + at, a.C, live);
-        fy.take(ystage, dout + at, a.C, live);
-        Decay d[TPG][VEC];
-        Affine<VEC> m = {}, r = {};
+        if (V::STAGED) {
+            copies_wait();
+            __syncwarp();
+        }
+        fg.take(gpart, gate + row, a.C, live, c - at.c0, at.inside);
+        fx.take(xpart, x + row, a.C, live, c - at.c0, at.inside);
+        fy.take(ypart, dout + row, a.C, live, c - at.c0, at.inside);
+        __syncwarp();
+        if (V::STAGED && u - V::WARPS >= at.first) ask(u - V::WARPS);
+        Decay<N> d[UNIT];
+        F<N> before[UNIT];
+        F<N> mg = all<N>(0.f), mb = mg;
         int q = marks.s;
 #pragma unroll
-        for (int i = 0; i < TPG; ++i) {
+        for (int i = 0; i < UNIT; ++i) {
+            const F<N> g = fg.r[i].get(), y = fx.r[i].get();
+            d[i] = Decay<N>::of(g);
+            mg = add(mg, g);
             if (FLAT && (marks.first >> i & 1)) {
                 if (i) q = Marks::next(a, q, t + i);
-                float f[VEC] = {};
-                if (a.init && inside) load_vec<VEC>(a.init + (size_t)q * a.C + c, f);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) { m.b[k] = f[k]; m.g[k] = -INFINITY; }
+                h = at.inside ? read_or_zero<N>(a.init, (size_t)q * a.C + c) : all<N>(0.f);
             }
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float g = fg.r[i].get(k);
-                d[i][k] = Decay::of(g);
-                const float y = fx.r[i].get(k);
-                m.g[k] += g;
-                r.g[k] += g;
-                m.b[k] = d[i][k].step(m.b[k], COMP ? d[i][k].complement() * y : y);
-            }
+            before[i] = h;
+            h = d[i].step(h, COMP ? mul(d[i].complement(), y) : y);
         }
-        // against time: the sequence of the last row first
-        int qlast = q;
-        if (FLAT && marks.last) {
+        const int qlast = q;   // against time: the sequence of the last row first
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) r.g[k] = -INFINITY;
-        }
-        q = qlast;
-#pragma unroll
-        for (int i = TPG - 1; i >= 0; --i) {
+        for (int i = UNIT - 1; i >= 0; --i) {
             if (FLAT && (marks.last >> i & 1)) {
-                float f[VEC] = {};
-                if (a.dfin && inside) load_vec<VEC>(a.dfin + (size_t)q * a.C + c, f);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) r.b[k] = f[k];
+                mb = at.inside ? read_or_zero<N>(a.dfin, (size_t)q * a.C + c) : all<N>(0.f);
+                mg = all<N>(-INFINITY);
             }
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) r.b[k] = d[i][k].times(fy.r[i].get(k) + r.b[k]);
+            mb = d[i].times(add(fy.r[i].get(), mb));
             if (FLAT && i && (marks.first >> i & 1)) q = previous(a, q);
         }
-        meet_warp<V, false, false>(m, inner, set);
-        meet_warp<V, true, true>(r, ex, set);
-        __syncthreads();
-        if (V::STAGED && step + 1 < steps) ask(step + 1);
-        if (a.span > 1) {
-            tell_walk<V, true>(ex, set, rank, a.span);
-            cluster_meet();
+        const Decay<N> md = Decay<N>::of(mg);
+        if (u + 1 < at.last) {
+            take_over(at.warp);
+            e = read<N>(&hand.state[at.warp][l]);
         }
-        float e[VEC], front[VEC];
-        fold<V, true>(base, e, front, ex, set, rank, a.span);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) e[k] = Decay::of(r.g[k]).step(e[k], r.b[k]);
-        for (int w = 0; w < (int)(threadIdx.x >> 5); ++w)
-            advance<VEC>(h, &inner.v[set][w][(lane % V::LANES) * VEC], &inner.b[set][w][(lane % V::LANES) * VEC]);
-        float before[TPG][VEC];
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) h[k] = Decay::of(m.g[k]).step(h[k], m.b[k]);
-        q = marks.s;
-#pragma unroll
-        for (int i = 0; i < TPG; ++i) {
-            if (FLAT && (marks.first >> i & 1)) {
-                if (i) q = Marks::next(a, q, t + i);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) h[k] = 0.f;
-                if (a.init && inside) load_vec<VEC>(a.init + (size_t)q * a.C + c, h);
-            }
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float y = fx.r[i].get(k);
-                before[i][k] = h[k];
-                h[k] = d[i][k].step(h[k], COMP ? d[i][k].complement() * y : y);
-            }
+        const F<N> behind = md.step(e, mb);
+        if (u > at.first) {
+            const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
+            write<N>(&hand.state[next][l], behind);
+            hand_on(next);
         }
-        q = qlast;
+        if (!FLAT && a.dinit && u == 0 && at.inside) write<N>(a.dinit + (size_t)at.s * a.C + c, behind);
+        if (plain) {
 #pragma unroll
-        for (int i = TPG - 1; i >= 0; --i) {
-            if (i < live) {
-                if (FLAT && (marks.last >> i & 1)) {
+            for (int i = UNIT - 1; i >= 0; --i) {
+                const F<N> dh = add(fy.r[i].get(), e);
+                e = d[i].times(dh);
+                write<N>(dx + row + (size_t)i * a.C, COMP ? mul(d[i].complement(), dh) : dh);
+                write<N>(dgate + row + (size_t)i * a.C, mul(COMP ? fma(fx.r[i].get(), all<N>(-1.f), before[i]) : before[i], e));
+            }
+        } else if (at.inside) {
+            q = qlast;
 #pragma unroll
-                    for (int k = 0; k < VEC; ++k) e[k] = 0.f;
-                    if (a.dfin) load_vec<VEC>(a.dfin + (size_t)q * a.C + c, e);
-                }
-                float px[VEC], pg[VEC];
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) {
-                    const float dh = fy.r[i].get(k) + e[k];
-                    e[k] = d[i][k].times(dh);
-                    px[k] = COMP ? d[i][k].complement() * dh : dh;
-                    pg[k] = (COMP ? before[i][k] - fx.r[i].get(k) : before[i][k]) * e[k];
-                }
-                store_vec<VEC>(dx + at + (size_t)i * a.C, px);
-                store_vec<VEC>(dgate + at + (size_t)i * a.C, pg);
+            for (int i = UNIT - 1; i >= 0; --i) {
+                if (i >= live) continue;
+                if (FLAT && (marks.last >> i & 1)) e = read_or_zero<N>(a.dfin, (size_t)q * a.C + c);
+                const F<N> dh = add(fy.r[i].get(), e);
+                e = d[i].times(dh);
+                write<N>(dx + row + (size_t)i * a.C, COMP ? mul(d[i].complement(), dh) : dh);
+                write<N>(dgate + row + (size_t)i * a.C, mul(COMP ? fma(fx.r[i].get(), all<N>(-1.f), before[i]) : before[i], e));
                 if (FLAT && (marks.first >> i & 1)) {
-                    if (a.dinit) store_vec<VEC>(a.dinit + (size_t)q * a.C + c, e);
+                    if (a.dinit) write<N>(a.dinit + (size_t)q * a.C + c, e);
                     if (i) q = previous(a, q);
                 }
             }
         }
     }
-    if (!FLAT && a.dinit && inside && rank == 0 && group == 0) store_vec<VEC>(a.dinit + (size_t)s * a.C + c, base);
+    if (SPLIT) cluster_wait();
 }
 
 // One thread per N channels of a sequence; the cached state is read and written once.
@@ -601,16 +660,16 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const T* x, const float*
         load_vec<N>(x + at, y);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const Decay d = Decay::of(g[j]);
-            h[j] = d.step(h[j], COMP ? d.complement() * y[j] : y[j]);
+            const Decay<1> d = Decay<1>::of({{g[j]}});
+            h[j] = d.step({{h[j]}}, {{COMP ? d.complement().x[0] * y[j] : y[j]}}).x[0];
         }
         store_vec<N>(out + at, h);
     }
     store_vec<N>(state + b * C + c, h);
 }
 
-// Sequences shorter than a tile are walked as one flat batch.
-bool is_flat(const osdn_scan_params& p) { return p.nseq > 0 || (p.B > 1 && p.T < TILE); }
+// Short sequences are walked as one flat batch.
+bool is_flat(const osdn_scan_params& p) { return p.nseq > 0 || (p.B > 1 && p.T < 64); }
 
 ScanArgs make_args(const osdn_scan_params& p)
 {
@@ -620,21 +679,24 @@ ScanArgs make_args(const osdn_scan_params& p)
     a.T = p.T;
     a.C = p.C;
     a.rows = p.nseq > 0 || !is_flat(p) ? p.T : p.B * p.T;
-    a.tiles = div_up(a.rows, TILE);
+    a.units = div_up(a.rows, UNIT);
     return a;
 }
 
-template <typename V> bool launch_walks(void (*kernel)(ScanArgs), ScanArgs a, bool flat, int row_bytes, size_t inner, cudaStream_t st)
+// Kernel(SPLIT) for the walks of a batch.  A walk is split until there is a CTA for each SM: its CTAs read their rows twice.
+template <typename V, typename K> bool launch_walks(K kernel, ScanArgs a, bool flat, int part, cudaStream_t st)
 {
     const long long walks = (long long)(flat ? 1 : a.S) * div_up(a.C, V::CB);
     a.span = 1;
-    while (a.span < MAX_SPAN && a.span < a.tiles && walks * a.span < 148 * 2) a.span *= 2;
-    const size_t smem = inner + (V::STAGED ? (size_t)TILE * V::CB * row_bytes : 0) + Exchange<V>::bytes(a.span);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
-    if (a.span > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
+    while (a.span < MAX_SPAN && a.units >= 2 * a.span * V::WARPS && walks * a.span < XCTA) a.span *= 2;
+    const bool split = a.span > 1;
+    const size_t smem = sizeof(Hand<V>) + (V::STAGED ? (size_t)V::WARPS * part : 0);
+    void (*f)(ScanArgs) = split ? kernel(std::true_type{}) : kernel(std::false_type{});
+    if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
+    if (a.span > 8 && cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(walks * a.span));
-    cfg.blockDim = dim3(V::THREADS);
+    cfg.blockDim = dim3(32 * V::WARPS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -644,17 +706,23 @@ template <typename V> bool launch_walks(void (*kernel)(ScanArgs), ScanArgs a, bo
     attr[1].val.clusterDim.x = a.span;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = a.span > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess;
+    cfg.numAttrs = split ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, f, a) == cudaSuccess;
 }
+
+template <typename T> bool is_wide(int C) { return C % (16 / (int)sizeof(T)) == 0; }   // rows in pieces of 16 bytes
 
 template <typename T, bool COMP> bool launch_forward(const ScanArgs& a, bool flat, cudaStream_t st)
 {
     auto go = [&](auto cover) {
         using V = decltype(cover);
-        return launch_walks<V>(flat ? scan_fwd_kernel<V, COMP, true> : scan_fwd_kernel<V, COMP, false>, a, flat, 4 + sizeof(T), 0, st);
+        auto kernel = [&](auto split) {
+            constexpr bool SPLIT = decltype(split)::value;
+            return flat ? scan_fwd_kernel<V, COMP, true, SPLIT> : scan_fwd_kernel<V, COMP, false, SPLIT>;
+        };
+        return launch_walks<V>(kernel, a, flat, Fetch<float, V>::BYTES + Fetch<T, V>::BYTES, st);
     };
-    return a.C % 4 == 0 ? go(Cover<T, 4, 16, 256>{}) : go(Cover<T, 1, 32, 256>{});
+    return is_wide<T>(a.C) ? go(Cover<T, 2, XW>{}) : go(Cover<T, 1, XW>{});
 }
 
 template <typename T, bool COMP> int run_backward(const ScanArgs& a, bool flat, bool saved, cudaStream_t st)
@@ -666,12 +734,13 @@ template <typename T, bool COMP> int run_backward(const ScanArgs& a, bool flat, 
     }
     auto go = [&](auto cover) {
         using V = decltype(cover);
-        return launch_walks<V>(flat ? scan_bwd_kernel<V, COMP, true> : scan_bwd_kernel<V, COMP, false>, a, flat, 4 + 2 * sizeof(T),
-                               sizeof(Inner<V>), st);
+        auto kernel = [&](auto split) {
+            constexpr bool SPLIT = decltype(split)::value;
+            return flat ? scan_bwd_kernel<V, COMP, true, SPLIT> : scan_bwd_kernel<V, COMP, false, SPLIT>;
+        };
+        return launch_walks<V>(kernel, a, flat, Fetch<float, V>::BYTES + 2 * Fetch<T, V>::BYTES, st);
     };
-    // fp32: twice the threads, half the rows each, for the registers that a row's values take
-    const bool ok = a.C % 4 == 0 ? go(Cover<T, 4, 16, 512>{}) : go(Cover<T, 1, 32, 256>{});
-    return ok ? n : -1;
+    return (is_wide<T>(a.C) ? go(Cover<T, 2, XW>{}) : go(Cover<T, 1, XW>{})) ? n : -1;
 }
 
 template <typename T, int N, bool COMP>
@@ -693,7 +762,7 @@ template <typename F> int by_type(const osdn_scan_params& p, F f)   // f(element
 size_t scan_workspace(const osdn_scan_params& p)
 {
     const ScanArgs a = make_args(p);
-    return align_up((size_t)(is_flat(p) ? 1 : p.B) * a.tiles * p.C * 4, 256);
+    return align_up((size_t)(is_flat(p) ? 1 : p.B) * a.units * p.C * 4, 256);
 }
 
 int scan_forward(const osdn_scan_params& p, const void* x, const float* gate, const float* init, void* out, float* fin,
