@@ -1,6 +1,18 @@
 // Short causal depthwise convolution over the tokens of a sequence: forward, backward, decode step.
 #include "osdn_rows.cuh"
 
+#ifndef XMF
+#define XMF 4
+#endif
+#ifndef XUF
+#define XUF 4
+#endif
+#ifndef XMB
+#define XMB 4
+#endif
+#ifndef XUB
+#define XUB 4
+#endif
 namespace osdn {
 namespace {
 
@@ -14,11 +26,24 @@ struct ConvArgs {
     long long walks;        // chunks of the whole batch
 };
 
-// Where results are rounded to bf16 (2^-9 of the value) the quick exponential and division (about 2^-21) are exact enough.
-template <typename T> __device__ __forceinline__ float sigmoid(float z)
+// z sigmoid(z) needs 1 / (1 + exp(-z)).  Where results are rounded to bf16 (2^-9 of the value) the hardware's exponential and
+// reciprocal (about 2^-21) are exact enough.
+template <typename T, int L> __device__ __forceinline__ F<L> sigmoid(const F<L>& z)
 {
-    if constexpr (sizeof(T) == 2) return __fdividef(1.f, 1.f + __expf(-z));
-    else return 1.f / (1.f + expf(-z));
+    F<L> s;
+    if constexpr (sizeof(T) == 2) {
+        const F<L> e = mul(z, all<L>(-1.44269504f));
+#pragma unroll
+        for (int k = 0; k < L; ++k) {
+            float x;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(e.x[k]));
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x[k]) : "f"(1.f + x));
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < L; ++k) s.x[k] = 1.f / (1.f + expf(-z.x[k]));
+    }
+    return s;
 }
 
 // Where a walk over the rows of one chunk stands: its sequence and the sequence's first row and end.
@@ -35,28 +60,35 @@ struct Place {
 
 // x row t of the sequence, or the state's row where t lies in front of it.
 template <typename T, int N, int W>
-__device__ __forceinline__ void row_before(const ConvArgs& a, const T* x, const Place& at, int t, int c, float (&v)[N])
+__device__ __forceinline__ Channels<T, N> row_before(const ConvArgs& a, const T* x, const Place& at, int t, int c)
 {
-    if (t >= at.start) {
-        load_vec<N>(x + (size_t)t * a.C + c, v);
-    } else if (a.init) {
-        load_vec<N>(static_cast<const T*>(a.init) + ((size_t)at.s * (W - 1) + (W - 1) + (t - at.start)) * a.C + c, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.f;
-    }
+    if (t >= at.start) return Channels<T, N>::load(x + (size_t)t * a.C + c);
+    if (!a.init) return Channels<T, N>::zero();
+    return Channels<T, N>::load(static_cast<const T*>(a.init) + ((size_t)at.s * (W - 1) + (W - 1) + (t - at.start)) * a.C + c);
 }
 
-template <typename T, int N, int W>
-__device__ __forceinline__ void load_taps(const ConvArgs& a, int c, float (&w)[W][N], float (&b)[N])
-{
+// The taps of N channels, in pairs: one after the other in memory, read in 16-byte pieces.
+template <int N, int W> struct Taps {
+    static constexpr int L = N % 2 == 0 ? 2 : 1, Q = N / L;
+    F<L> w[W][Q], b[Q];
+    __device__ __forceinline__ void load(const float* weight, const float* bias, int c)
+    {
+        float f[N * W], g[N];
+        load_vec<N * W>(weight + (size_t)c * W, f);
+        if (bias) {
+            load_vec<N>(bias + c, g);
+        } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
+            for (int j = 0; j < N; ++j) g[j] = 0.f;
+        }
 #pragma unroll
-        for (int i = 0; i < W; ++i) w[i][j] = a.w[(size_t)(c + j) * W + i];
-        b[j] = a.bias ? a.bias[c + j] : 0.f;
+        for (int j = 0; j < N; ++j) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i][j / L].x[j % L] = f[j * W + i];
+            b[j / L].x[j % L] = g[j];
+        }
     }
-}
+};
 
 // A state of an empty sequence (or its gradient) passes through.
 template <typename T, int N, int W>
@@ -66,18 +98,39 @@ __device__ __forceinline__ void pass_empty(const ConvArgs& a, const void* from, 
     for (long long s = walk; s < a.rows.S; s += a.walks) {
         if (a.rows.cu[s + 1] > a.rows.cu[s]) continue;
         for (int i = 0; i < W - 1; ++i) {
-            float v[N] = {};
             const size_t at = ((size_t)s * (W - 1) + i) * a.C + c;
-            if (from) load_vec<N>(static_cast<const T*>(from) + at, v);
-            store_vec<N>(static_cast<T*>(to) + at, v);
+            (from ? Channels<T, N>::load(static_cast<const T*>(from) + at) : Channels<T, N>::zero()).store(static_cast<T*>(to) + at);
         }
     }
 }
 
+// One output row from the window of the rows before it (oldest first) and its own; the window moves on.
 template <typename T, int N, int W, bool SILU>
-__global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a)
+__device__ __forceinline__ Channels<T, N> convolve(const Taps<N, W>& k, F<Taps<N, W>::L> (&prev)[W - 1][Taps<N, W>::Q], const Channels<T, N>& row)
+{
+    Channels<T, N> y;
+#pragma unroll
+    for (int q = 0; q < Taps<N, W>::Q; ++q) {
+        const auto v = row.get(q);
+        auto z = k.b[q];
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) z = fma(k.w[j][q], prev[j][q], z);
+        z = fma(k.w[W - 1][q], v, z);
+        y.set(q, SILU ? mul(z, sigmoid<T>(z)) : z);
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j) prev[j][q] = prev[j + 1][q];
+        prev[W - 2][q] = v;
+    }
+    return y;
+}
+
+// A thread walks the rows of a chunk over N channels, U rows on their way at a time.
+template <typename T, int N, int W, bool SILU>
+__global__ void __launch_bounds__(128, XMF) conv_fwd_kernel(ConvArgs a)
 {
     pdl_wait();
+    using Row = Channels<T, N>;
+    constexpr int Q = Row::Q, U = XUF;
     const int n = a.C / N;
     const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     if (i >= a.walks * n) return;
@@ -92,61 +145,72 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a)
     const T* x = static_cast<const T*>(a.x) + base;
     T* out = static_cast<T*>(a.out) + base;
     at.enter(a.rows, t0, limit);
-    float w[W][N], b[N], prev[W - 1][N];
-    load_taps<T, N, W>(a, c, w, b);
+    Taps<N, W> k;
+    k.load(a.w, a.bias, c);
+    F<Row::L> prev[W - 1][Q];
+    auto refill = [&](int t) {
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) row_before<T, N, W>(a, x, at, t0 - (W - 1) + j, c, prev[j]);
-    constexpr int U = 4;
+        for (int j = 0; j < W - 1; ++j) {
+            const Row r = row_before<T, N, W>(a, x, at, t - (W - 1) + j, c);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) prev[j][q] = r.get(q);
+        }
+    };
+    refill(t0);
     for (int t = t0; t < t1; t += U) {
-        float v[U][N];
+        Row v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (t + u < t1) load_vec<N>(x + (size_t)(t + u) * a.C + c, v[u]);
+            if (t + u < t1) v[u] = Row::load(x + (size_t)(t + u) * a.C + c);
+        if (t + U <= t1 && t + U < at.end) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (t + u >= t1) break;
-            if (t + u >= at.end) {   // the next sequence that is not empty
-                at.enter(a.rows, t + u, limit);
+            for (int u = 0; u < U; ++u) convolve<T, N, W, SILU>(k, prev, v[u]).store(out + (size_t)(t + u) * a.C + c);
+        } else {
 #pragma unroll
-                for (int j = 0; j < W - 1; ++j) row_before<T, N, W>(a, x, at, t + u - (W - 1) + j, c, prev[j]);
+            for (int u = 0; u < U; ++u) {
+                if (t + u >= t1) break;
+                if (t + u >= at.end) {   // the next sequence that is not empty
+                    at.enter(a.rows, t + u, limit);
+                    refill(t + u);
+                }
+                convolve<T, N, W, SILU>(k, prev, v[u]).store(out + (size_t)(t + u) * a.C + c);
+                if (a.fin && t + u + 1 == at.end)
+#pragma unroll
+                    for (int j = 0; j < W - 1; ++j) {
+                        Row r;
+#pragma unroll
+                        for (int q = 0; q < Q; ++q) r.set(q, prev[j][q]);
+                        r.store(static_cast<T*>(a.fin) + ((size_t)at.s * (W - 1) + j) * a.C + c);
+                    }
             }
-            float z[N];
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                float y = b[k];
-#pragma unroll
-                for (int j = 0; j < W - 1; ++j) y = fmaf(w[j][k], prev[j][k], y);
-                y = fmaf(w[W - 1][k], v[u][k], y);
-                z[k] = SILU ? y * sigmoid<T>(y) : y;
-#pragma unroll
-                for (int j = 0; j + 1 < W - 1; ++j) prev[j][k] = prev[j + 1][k];
-                prev[W - 2][k] = v[u][k];
-            }
-            store_vec<N>(out + (size_t)(t + u) * a.C + c, z);
-            if (a.fin && t + u + 1 == at.end)
-#pragma unroll
-                for (int j = 0; j < W - 1; ++j)
-                    store_vec<N>(static_cast<T*>(a.fin) + ((size_t)at.s * (W - 1) + j) * a.C + c, prev[j]);
         }
     }
 }
 
-// A thread walks the tokens of its chunk and, for the gradients of the chunk's last rows, up to W-1 behind it.  acc[j] is the
+// A thread walks the rows of its chunk and, for the gradients of the chunk's last rows, up to W-1 behind it.  acc[j] is the
 // gradient, so far, of row t - (W-1) + j; it is complete once dz_t is in, or at the sequence's end, where all W-1 last rows
 // take the gradient of the state as well.  Rows in front of a sequence are its state's.
 template <typename T, int N, int W, bool SILU>
-__global__ void __launch_bounds__(128) conv_bwd_kernel(ConvArgs a, int gx)
+__global__ void __launch_bounds__(128, XMB) conv_bwd_kernel(ConvArgs a, int gx)
 {
     extern __shared__ float sums[];   // [128 / gx][W + 1][gx * N]
     pdl_wait();
+    using Row = Channels<T, N>;
+    constexpr int Q = Row::Q, L = Row::L, U = XUB;
     const int n = a.C / N;
     const int lane = threadIdx.x % gx, row = threadIdx.x / gx, rows = blockDim.x / gx;
     const int group = blockIdx.x * gx + lane;
     const int c = group * N;
-    float dw[W][N] = {}, db[N] = {};
+    F<L> dw[W][Q], db[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) dw[j][q] = all<L>(0.f);
+        db[q] = all<L>(0.f);
+    }
     if (group < n) {
-        float w[W][N], b[N];
-        load_taps<T, N, W>(a, c, w, b);
+        Taps<N, W> k;
+        k.load(a.w, a.bias, c);
         const int limit = a.rows.cu ? rows_end(a.rows) : a.rows.T;
         for (long long walk = (long long)blockIdx.y * rows + row; walk < a.walks; walk += (long long)gridDim.y * rows) {
             pass_empty<T, N, W>(a, a.dfin, a.dinit, walk, c);
@@ -158,69 +222,109 @@ __global__ void __launch_bounds__(128) conv_bwd_kernel(ConvArgs a, int gx)
             const T* dout = static_cast<const T*>(a.dout) + base;
             T* dx = static_cast<T*>(a.dx) + base;
             at.enter(a.rows, t0, limit);
-            float prev[W - 1][N], acc[W][N] = {};
+            F<L> prev[W - 1][Q], acc[W][Q];
+            auto refill = [&](int t) {
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) row_before<T, N, W>(a, x, at, t0 - (W - 1) + j, c, prev[j]);
-            auto put = [&](int t, const float (&v)[N]) {   // the gradient of row t is complete
-                if (t >= at.start) {
-                    if (t >= t0 && t < t1) store_vec<N>(dx + (size_t)t * a.C + c, v);
-                } else if (a.dinit && at.start >= t0 && at.start < t1) {
-                    store_vec<N>(static_cast<T*>(a.dinit) + ((size_t)at.s * (W - 1) + (W - 1) + (t - at.start)) * a.C + c, v);
+                for (int j = 0; j < W - 1; ++j) {
+                    const Row r = row_before<T, N, W>(a, x, at, t - (W - 1) + j, c);
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) {
+                        prev[j][q] = r.get(q);
+                        acc[j][q] = all<L>(0.f);
+                    }
                 }
             };
-            for (int t = t0; t < t1 + W - 1 && t < limit; ++t) {
-                if (t >= at.end) {
-                    if (t >= t1) break;
-                    at.enter(a.rows, t, limit);
+            refill(t0);
+            auto put = [&](int t, const F<L> (&v)[Q]) {   // the gradient of row t is complete
+                Row r;
 #pragma unroll
-                    for (int j = 0; j < W - 1; ++j) {
-                        row_before<T, N, W>(a, x, at, t - (W - 1) + j, c, prev[j]);
-#pragma unroll
-                        for (int k = 0; k < N; ++k) acc[j][k] = 0.f;
-                    }
+                for (int q = 0; q < Q; ++q) r.set(q, v[q]);
+                if (t >= at.start) {
+                    if (t >= t0 && t < t1) r.store(dx + (size_t)t * a.C + c);
+                } else if (a.dinit && at.start >= t0 && at.start < t1) {
+                    r.store(static_cast<T*>(a.dinit) + ((size_t)at.s * (W - 1) + (W - 1) + (t - at.start)) * a.C + c);
                 }
-                float v[N], g[N];
-                load_vec<N>(x + (size_t)t * a.C + c, v);
-                load_vec<N>(dout + (size_t)t * a.C + c, g);
-                const bool own = t < t1;
+            };
+            auto take = [&](const Row& xr, const Row& gr, bool own) {   // dz of one row into the sums and the window
 #pragma unroll
-                for (int k = 0; k < N; ++k) {
+                for (int q = 0; q < Q; ++q) {
+                    const F<L> v = xr.get(q);
+                    F<L> g = gr.get(q);
                     if (SILU) {
-                        float z = b[k];
+                        F<L> z = k.b[q];
 #pragma unroll
-                        for (int j = 0; j < W - 1; ++j) z = fmaf(w[j][k], prev[j][k], z);
-                        z = fmaf(w[W - 1][k], v[k], z);
-                        const float s = sigmoid<T>(z);
-                        g[k] *= s * fmaf(z, 1.f - s, 1.f);
+                        for (int j = 0; j < W - 1; ++j) z = fma(k.w[j][q], prev[j][q], z);
+                        z = fma(k.w[W - 1][q], v, z);
+                        const F<L> s = sigmoid<T>(z);
+                        g = mul(g, mul(s, fma(z, fma(s, all<L>(-1.f), all<L>(1.f)), all<L>(1.f))));
                     }
-                    const float d = own ? g[k] : 0.f;
-                    db[k] += d;
+                    if (own) {
+                        db[q] = add(db[q], g);
 #pragma unroll
-                    for (int j = 0; j < W - 1; ++j) {
-                        dw[j][k] = fmaf(d, prev[j][k], dw[j][k]);
-                        acc[j][k] = fmaf(w[j][k], g[k], acc[j][k]);
+                        for (int j = 0; j < W - 1; ++j) dw[j][q] = fma(g, prev[j][q], dw[j][q]);
+                        dw[W - 1][q] = fma(g, v, dw[W - 1][q]);
                     }
-                    dw[W - 1][k] = fmaf(d, v[k], dw[W - 1][k]);
-                    acc[W - 1][k] = w[W - 1][k] * g[k];
 #pragma unroll
-                    for (int j = 0; j + 1 < W - 1; ++j) prev[j][k] = prev[j + 1][k];
-                    prev[W - 2][k] = v[k];
+                    for (int j = 0; j < W - 1; ++j) acc[j][q] = fma(k.w[j][q], g, acc[j][q]);
+                    acc[W - 1][q] = mul(k.w[W - 1][q], g);
+#pragma unroll
+                    for (int j = 0; j + 1 < W - 1; ++j) prev[j][q] = prev[j + 1][q];
+                    prev[W - 2][q] = v;
                 }
-                put(t - (W - 1), acc[0]);
+            };
+            auto shift = [&] {
 #pragma unroll
                 for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-                    for (int k = 0; k < N; ++k) acc[j][k] = acc[j + 1][k];
-                if (t + 1 == at.end) {
+                    for (int q = 0; q < Q; ++q) acc[j][q] = acc[j + 1][q];
+            };
+            const int tend = min(t1 + W - 1, limit);
+            bool over = false;
+            for (int t = t0; t < tend && !over; t += U) {
+                Row xv[U], gv[U];
 #pragma unroll
-                    for (int j = 0; j < W - 1; ++j) {
-                        if (a.dfin) {
-                            float f[N];
-                            load_vec<N>(static_cast<const T*>(a.dfin) + ((size_t)at.s * (W - 1) + j) * a.C + c, f);
+                for (int u = 0; u < U; ++u)
+                    if (t + u < tend) {
+                        xv[u] = Row::load(x + (size_t)(t + u) * a.C + c);
+                        gv[u] = Row::load(dout + (size_t)(t + u) * a.C + c);
+                    }
+                if (t + U <= t1 && t + U < at.end && t - (W - 1) >= t0 && t - (W - 1) >= at.start) {
 #pragma unroll
-                            for (int k = 0; k < N; ++k) acc[j][k] += f[k];
+                    for (int u = 0; u < U; ++u) {
+                        take(xv[u], gv[u], true);
+                        Row r;
+#pragma unroll
+                        for (int q = 0; q < Q; ++q) r.set(q, acc[0][q]);
+                        r.store(dx + (size_t)(t + u - (W - 1)) * a.C + c);
+                        shift();
+                    }
+                } else {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int s = t + u;
+                        if (s >= tend || over) continue;
+                        if (s >= at.end) {
+                            if (s >= t1) {
+                                over = true;
+                                continue;
+                            }
+                            at.enter(a.rows, s, limit);
+                            refill(s);
                         }
-                        put(t - (W - 2) + j, acc[j]);
+                        take(xv[u], gv[u], s < t1);
+                        put(s - (W - 1), acc[0]);
+                        shift();
+                        if (s + 1 == at.end) {
+#pragma unroll
+                            for (int j = 0; j < W - 1; ++j) {
+                                if (a.dfin) {
+                                    const Row f = Row::load(static_cast<const T*>(a.dfin) + ((size_t)at.s * (W - 1) + j) * a.C + c);
+#pragma unroll
+                                    for (int q = 0; q < Q; ++q) acc[j][q] = add(acc[j][q], f.get(q));
+                                }
+                                put(s - (W - 2) + j, acc[j]);
+                            }
+                        }
                     }
                 }
             }
@@ -229,10 +333,10 @@ __global__ void __launch_bounds__(128) conv_bwd_kernel(ConvArgs a, int gx)
     // the block's sums, row by row in order
     float* mine = sums + (size_t)row * (W + 1) * gx * N;
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
+    for (int m = 0; m < N; ++m) {
 #pragma unroll
-        for (int j = 0; j < W; ++j) mine[(j * gx + lane) * N + k] = dw[j][k];
-        mine[(W * gx + lane) * N + k] = db[k];
+        for (int j = 0; j < W; ++j) mine[(j * gx + lane) * N + m] = dw[j][m / L].x[m % L];
+        mine[(W * gx + lane) * N + m] = db[m / L].x[m % L];
     }
     __syncthreads();
     const int width = gx * N;
@@ -244,41 +348,39 @@ __global__ void __launch_bounds__(128) conv_bwd_kernel(ConvArgs a, int gx)
     }
 }
 
+// A thread keeps the taps of N channels and takes `each` sequences one after the other.
 template <typename T, int N, int W, bool SILU>
 __global__ void __launch_bounds__(128) conv_step_kernel(const T* x, const float* weight, const float* bias, T* state, T* out, int B,
-                                                        int L, int C)
+                                                        int len, int C, int each)
 {
     pdl_wait();
+    using Row = Channels<T, N>;
+    constexpr int Q = Row::Q;
     const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     const int n = C / N;
-    if (i >= (long long)B * n) return;
-    const size_t s = i / n;
+    const long long first = i / n * each;
+    if (first >= B) return;
     const int c = (int)(i % n) * N;
-    ConvArgs a{};
-    a.w = weight; a.bias = bias; a.C = C;
-    float w[W][N], b[N], prev[W - 1][N];
-    load_taps<T, N, W>(a, c, w, b);
+    Taps<N, W> k;
+    k.load(weight, bias, c);
+    for (long long s = first; s < first + each && s < B; ++s) {
+        F<Row::L> prev[W - 1][Q];
+        Row r[W - 1];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) load_vec<N>(state + (s * (W - 1) + j) * C + c, prev[j]);
-    for (int t = 0; t < L; ++t) {
-        float v[N];
-        load_vec<N>(x + (s * L + t) * C + c, v);
-        float z[N];
+        for (int j = 0; j < W - 1; ++j) r[j] = Row::load(state + (s * (W - 1) + j) * C + c);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            float y = b[k];
+        for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) y = fmaf(w[j][k], prev[j][k], y);
-            y = fmaf(w[W - 1][k], v[k], y);
-            z[k] = SILU ? y * sigmoid<T>(y) : y;
+            for (int q = 0; q < Q; ++q) prev[j][q] = r[j].get(q);
+        for (int t = 0; t < len; ++t)
+            convolve<T, N, W, SILU>(k, prev, Row::load(x + (s * len + t) * C + c)).store(out + (s * len + t) * C + c);
 #pragma unroll
-            for (int j = 0; j + 1 < W - 1; ++j) prev[j][k] = prev[j + 1][k];
-            prev[W - 2][k] = v[k];
+        for (int j = 0; j < W - 1; ++j) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) r[j].set(q, prev[j][q]);
+            r[j].store(state + (s * (W - 1) + j) * C + c);
         }
-        store_vec<N>(out + (s * L + t) * C + c, z);
     }
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) store_vec<N>(state + (s * (W - 1) + j) * C + c, prev[j]);
 }
 
 template <typename F> int by_type(const osdn_conv_params& p, F f)   // f(element, taps, activation)
@@ -293,15 +395,22 @@ template <typename F> int by_type(const osdn_conv_params& p, F f)   // f(element
 }
 
 // Chunks of a walk: long ones read fewer rows twice, short ones make more threads.
-void plan_walks(ConvArgs& a, const osdn_conv_params& p, int N)
+void plan_walks(ConvArgs& a, const osdn_conv_params& p, int N, int longest)
 {
     const long long rows = (long long)p.B * p.T, n = p.C / N;
-    int chunk = 64;
-    while (chunk > 8 && rows * n / chunk < 148ll * 1024) chunk /= 2;
+    int chunk = longest;
+    while (chunk > 8 && rows * n / chunk < 148ll * 512) chunk /= 2;
     a.chunk = chunk;
     a.chunks = div_up(p.T, chunk);
     a.walks = (long long)(p.nseq > 0 ? 1 : p.B) * a.chunks;
 }
+#ifndef XLF
+#define XLF 32
+#endif
+#ifndef XLB
+#define XLB 64
+#endif
+constexpr int FWD_CHUNK = XLF, BWD_CHUNK = XLB;
 
 ConvArgs make_args(const osdn_conv_params& p)
 {
@@ -324,8 +433,8 @@ BwdPlan plan_backward(const ConvArgs& a, const osdn_conv_params& p, int N)
     while (b.gx > 1 && b.gx / 2 >= n) b.gx /= 2;
     b.grid_x = div_up(n, b.gx);
     const long long blocks = (a.walks + 128 / b.gx - 1) / (128 / b.gx);
-    const long long most = std::max(1, 148 * 4 / b.grid_x);
-    b.grid_y = (int)std::min(blocks, most);
+    const long long most = std::max(1, 148 * 4 / b.grid_x), rounds = (blocks + most - 1) / most;
+    b.grid_y = (int)((blocks + rounds - 1) / rounds);   // the same number of walks for every thread
     return b;
 }
 int backward_vec(const osdn_conv_params& p) { return p.C % 4 == 0 ? 4 : 1; }
@@ -362,7 +471,7 @@ bool launch_sum_rows(const float* part, int G, int C, int W, int M, float* out0,
 size_t conv_workspace(const osdn_conv_params& p)
 {
     ConvArgs a = make_args(p);
-    plan_walks(a, p, backward_vec(p));
+    plan_walks(a, p, backward_vec(p), BWD_CHUNK);
     return align_up((size_t)plan_backward(a, p, backward_vec(p)).grid_y * (p.W + 1) * p.C * 4, 256);
 }
 
@@ -378,7 +487,7 @@ int conv_forward(const osdn_conv_params& p, const void* x, const float* w, const
         constexpr bool SILU = decltype(act)::value;
         auto go = [&](auto vec) {
             constexpr int N = decltype(vec)::value;
-            plan_walks(a, p, N);
+            plan_walks(a, p, N, FWD_CHUNK);
             return launch_after(conv_fwd_kernel<T, N, W, SILU>, dim3(div_up(a.walks * (p.C / N), 128)), dim3(128), 0, st, a) ? 1 : -1;
         };
         return p.C % kWide<T> == 0 ? go(std::integral_constant<int, kWide<T>>{}) : go(std::integral_constant<int, 1>{});
@@ -400,7 +509,7 @@ int conv_backward(const osdn_conv_params& p, const void* x, const float* w, cons
         constexpr bool SILU = decltype(act)::value;
         auto go = [&](auto vec) {
             constexpr int N = decltype(vec)::value;
-            plan_walks(a, p, N);
+            plan_walks(a, p, N, BWD_CHUNK);
             const BwdPlan b = plan_backward(a, p, N);
             const size_t smem = (size_t)128 * (W + 1) * N * 4;
             if (!launch_after(conv_bwd_kernel<T, N, W, SILU>, dim3(b.grid_x, b.grid_y), dim3(128), smem, st, a, b.gx)) return -1;
@@ -422,8 +531,10 @@ int conv_step(const osdn_conv_params& p, const void* x, const float* w, const fl
         constexpr bool SILU = decltype(act)::value;
         auto go = [&](auto vec) {
             constexpr int N = decltype(vec)::value;
-            return launch_after(conv_step_kernel<T, N, W, SILU>, dim3(div_up((long long)p.B * (p.C / N), 128)), dim3(128), 0, st,
-                                static_cast<const T*>(x), w, bias, static_cast<T*>(state), static_cast<T*>(out), p.B, p.T, p.C)
+            const long long n = p.C / N;
+            const int each = (int)std::max(1ll, std::min(4ll, p.B * n / (148 * 256)));   // the taps are as many bytes as a row
+            return launch_after(conv_step_kernel<T, N, W, SILU>, dim3(div_up(div_up(p.B, each) * n, 128)), dim3(128), 0, st,
+                                static_cast<const T*>(x), w, bias, static_cast<T*>(state), static_cast<T*>(out), p.B, p.T, p.C, each)
                        ? 1 : -1;
         };
         return p.C % kWide<T> == 0 ? go(std::integral_constant<int, kWide<T>>{}) : go(std::integral_constant<int, 1>{});

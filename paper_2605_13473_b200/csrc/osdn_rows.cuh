@@ -101,6 +101,128 @@ template <int N> __device__ __forceinline__ void store_vec(__nv_bfloat16* p, con
     }
 }
 
+// N channels at once; two go through the packed fp32 instructions.
+template <int N> struct F {
+    float x[N];
+};
+__device__ __forceinline__ unsigned long long pack(const F<2>& a)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x[0]), "f"(a.x[1]));
+    return r;
+}
+__device__ __forceinline__ F<2> unpack(unsigned long long r)
+{
+    F<2> a;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a.x[0]), "=f"(a.x[1]) : "l"(r));
+    return a;
+}
+template <int N> __device__ __forceinline__ F<N> all(float v)
+{
+    F<N> a;
+#pragma unroll
+    for (int k = 0; k < N; ++k) a.x[k] = v;
+    return a;
+}
+template <int N> __device__ __forceinline__ F<N> fma(const F<N>& a, const F<N>& b, const F<N>& c)
+{
+    if constexpr (N == 2) {
+        unsigned long long d;
+        asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)), "l"(pack(c)));
+        return unpack(d);
+    } else {
+        return {{fmaf(a.x[0], b.x[0], c.x[0])}};
+    }
+}
+template <int N> __device__ __forceinline__ F<N> add(const F<N>& a, const F<N>& b)
+{
+    if constexpr (N == 2) {
+        unsigned long long d;
+        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)));
+        return unpack(d);
+    } else {
+        return {{a.x[0] + b.x[0]}};
+    }
+}
+template <int N> __device__ __forceinline__ F<N> mul(const F<N>& a, const F<N>& b)
+{
+    if constexpr (N == 2) {
+        unsigned long long d;
+        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)));
+        return unpack(d);
+    } else {
+        return {{a.x[0] * b.x[0]}};
+    }
+}
+
+// N consecutive channels as they come from memory, in pairs (N = 1: alone).
+template <typename T, int N> struct Channels {
+    static constexpr int L = N % 2 == 0 ? 2 : 1, Q = N / L;
+    static constexpr int WORDS = N * (int)sizeof(T) / 4 > 0 ? N * (int)sizeof(T) / 4 : 1;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ static Channels zero()
+    {
+        Channels c;
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) c.w[i] = 0;
+        return c;
+    }
+    __device__ __forceinline__ static Channels load(const T* p)
+    {
+        Channels c;
+        if constexpr (WORDS % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < WORDS / 4; ++i) {
+                const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+                c.w[4 * i] = v.x; c.w[4 * i + 1] = v.y; c.w[4 * i + 2] = v.z; c.w[4 * i + 3] = v.w;
+            }
+        } else if constexpr (WORDS == 2) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            c.w[0] = v.x; c.w[1] = v.y;
+        } else if constexpr (sizeof(T) == 2 && N == 1) {
+            c.w[0] = *reinterpret_cast<const uint16_t*>(p);
+        } else {
+            c.w[0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+        return c;
+    }
+    __device__ __forceinline__ F<L> get(int q) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            if constexpr (L == 2) return {{__uint_as_float(w[2 * q]), __uint_as_float(w[2 * q + 1])}};
+            else return {{__uint_as_float(w[q])}};
+        } else {
+            if constexpr (L == 2) return {{__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xffff0000u)}};
+            else return {{__uint_as_float(w[q] << 16)}};
+        }
+    }
+    __device__ __forceinline__ void set(int q, const F<L>& v)
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int k = 0; k < L; ++k) w[L * q + k] = __float_as_uint(v.x[k]);
+        } else if constexpr (L == 2) {
+            w[q] = pair_bf16(v.x[0], v.x[1]);
+        } else {
+            const __nv_bfloat16 h = __float2bfloat16_rn(v.x[0]);
+            w[q] = *reinterpret_cast<const uint16_t*>(&h);
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+        if constexpr (WORDS % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        } else if constexpr (WORDS == 2) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        } else if constexpr (sizeof(T) == 2 && N == 1) {
+            *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+        } else {
+            *reinterpret_cast<uint32_t*>(p) = w[0];
+        }
+    }
+};
+
 inline int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // Entry points of the kernels' files.  The number of launches, or -1 on a launch error.

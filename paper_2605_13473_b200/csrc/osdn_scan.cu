@@ -3,76 +3,10 @@
 
 #include "osdn_rows.cuh"
 
-#ifndef XCTA
-#define XCTA 120
-#endif
-#ifndef XW
-#define XW 16
-#endif
-#ifndef XFMIN
-#define XFMIN 16
-#endif
-#ifndef XBMIN
-#define XBMIN 16
-#endif
 namespace osdn {
 namespace {
 
 constexpr int UNIT = 8;   // rows that a warp takes at a time; the forward keeps the state in front of each such stretch for the backward
-
-// N channels at once; two go through the packed fp32 instructions.
-template <int N> struct F {
-    float x[N];
-};
-__device__ __forceinline__ unsigned long long pack(const F<2>& a)
-{
-    unsigned long long r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x[0]), "f"(a.x[1]));
-    return r;
-}
-__device__ __forceinline__ F<2> unpack(unsigned long long r)
-{
-    F<2> a;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(a.x[0]), "=f"(a.x[1]) : "l"(r));
-    return a;
-}
-template <int N> __device__ __forceinline__ F<N> all(float v)
-{
-    F<N> a;
-#pragma unroll
-    for (int k = 0; k < N; ++k) a.x[k] = v;
-    return a;
-}
-template <int N> __device__ __forceinline__ F<N> fma(const F<N>& a, const F<N>& b, const F<N>& c)
-{
-    if constexpr (N == 2) {
-        unsigned long long d;
-        asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)), "l"(pack(c)));
-        return unpack(d);
-    } else {
-        return {{fmaf(a.x[0], b.x[0], c.x[0])}};
-    }
-}
-template <int N> __device__ __forceinline__ F<N> add(const F<N>& a, const F<N>& b)
-{
-    if constexpr (N == 2) {
-        unsigned long long d;
-        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)));
-        return unpack(d);
-    } else {
-        return {{a.x[0] + b.x[0]}};
-    }
-}
-template <int N> __device__ __forceinline__ F<N> mul(const F<N>& a, const F<N>& b)
-{
-    if constexpr (N == 2) {
-        unsigned long long d;
-        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack(a)), "l"(pack(b)));
-        return unpack(d);
-    } else {
-        return {{a.x[0] * b.x[0]}};
-    }
-}
 
 // exp(g) for g <= 0 as the sum of two floats, hi the nearest one to it:
 //   |g| <= 1/4:  from expm1(g) by its Taylor series to g^6 (remainder below 5e-8 of it): the sum keeps the distance from one;
@@ -121,9 +55,10 @@ struct ScanArgs {
 };
 
 // How a CTA covers its rows: its warps take units in turn, over CB channels, VEC to a lane.
-template <typename T_, int VEC_, int WARPS_> struct Cover {
+template <typename T_, int VEC_, int WARPS_, int DEPTH_> struct Cover {
     using T = T_;
-    static constexpr int VEC = VEC_, WARPS = WARPS_, CB = 32 * VEC, TPG = UNIT;
+    static_assert(WARPS_ <= 16, "a named barrier for each warp");
+    static constexpr int VEC = VEC_, WARPS = WARPS_, DEPTH = DEPTH_, CB = 32 * VEC, TPG = UNIT;
     static constexpr bool STAGED = VEC == 2;   // a warp's next unit is on its way in shared memory while it computes one
 };
 constexpr int MAX_SPAN = 16;
@@ -168,7 +103,9 @@ __device__ __forceinline__ void copy_async16(void* smem, const void* src, bool r
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(src),
                  "r"(real ? 16 : 0) : "memory");   // what is not there is filled with zeros
 }
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// A warp's units come in through DEPTH places of shared memory: one group of copies a unit, empty ones too.
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LATER> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory"); }
 
 // A warp's TPG rows of one tensor.  Staged: the warp copies them in 16-byte pieces to its own part of shared memory.
 template <typename E, typename V> struct Fetch {
@@ -273,9 +210,41 @@ template <int N> __device__ __forceinline__ F<N> read_remote(const float* mine, 
     else asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(a.x[0]) : "r"(at) : "memory");
     return a;
 }
-// One warp announces, another one waits: named barriers of 64 threads.
+// One warp announces, the next one waits: a named barrier of 64 threads for each warp that waits.  A CTA has sixteen of them
+// (with a number shared by two warps both may wait on it at once, and take one another for the announcement).
 __device__ __forceinline__ void hand_on(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ void take_over(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+// Both at once, the state stepped in between: h from `mine`, a h + b to `next`.  One block of instructions, because this is
+// what every warp of a walk waits for: left to itself the compiler puts work for later rows in between (forward of 8 x 2048
+// tokens, 1024 channels: 28 to 41 us with how it happened to be scheduled).
+template <int N>
+__device__ __forceinline__ F<N> relay(int id, int next_id, const float* mine, float* next, const Decay<N>& d, const F<N>& b, F<N>& behind)
+{
+    const uint32_t from = (uint32_t)__cvta_generic_to_shared(mine), to = (uint32_t)__cvta_generic_to_shared(next);
+    if constexpr (N == 2) {
+        unsigned long long h, t;
+        asm volatile("bar.sync %2, 64;\n\t"
+                     "ld.shared.b64 %0, [%3];\n\t"
+                     "fma.rn.f32x2 %1, %6, %0, %7;\n\t"
+                     "fma.rn.f32x2 %1, %5, %0, %1;\n\t"
+                     "st.shared.b64 [%4], %1;\n\t"
+                     "bar.arrive %8, 64;"
+                     : "=&l"(h), "=&l"(t) : "r"(id), "r"(from), "r"(to), "l"(pack(d.hi)), "l"(pack(d.lo)), "l"(pack(b)), "r"(next_id) : "memory");
+        behind = unpack(t);
+        return unpack(h);
+    } else {
+        float h, t;
+        asm volatile("bar.sync %2, 64;\n\t"
+                     "ld.shared.f32 %0, [%3];\n\t"
+                     "fma.rn.f32 %1, %6, %0, %7;\n\t"
+                     "fma.rn.f32 %1, %5, %0, %1;\n\t"
+                     "st.shared.f32 [%4], %1;\n\t"
+                     "bar.arrive %8, 64;"
+                     : "=&f"(h), "=&f"(t) : "r"(id), "r"(from), "r"(to), "f"(d.hi.x[0]), "f"(d.lo.x[0]), "f"(b.x[0]), "r"(next_id) : "memory");
+        behind = {{t}};
+        return {{h}};
+    }
+}
 
 // The sequence in front of q that is not empty (one there is: q does not begin the rows).
 __device__ __forceinline__ int previous(const ScanArgs& a, int q)
@@ -327,7 +296,7 @@ template <typename V, bool FLAT, bool SPLIT> struct Stand {
 // the other CTAs' the state in front of this one.  REVERSE: for e = a (y + e), from the end.  Warp 0 has the result.
 template <typename V, bool COMP, bool FLAT, bool REVERSE, typename S>
 __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& at, Hand<V>& hand, F<V::VEC> h, const float* gate,
-                                                    const typename V::T* x, char* gpart, char* xpart)
+                                                    const typename V::T* x, char* part, int bytes)
 {
     using FetchG = Fetch<float, V>;
     using FetchX = Fetch<typename V::T, V>;
@@ -335,15 +304,20 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
     const int l = (threadIdx.x & 31) * N, per = (at.last - at.first + V::WARPS - 1) / V::WARPS;
     const int lo = min(at.first + at.warp * per, at.last), hi = min(lo + per, at.last);
     auto unit = [&](int i) { return REVERSE ? hi - 1 - i : lo + i; };
-    auto ask = [&](int i) {
-        const int t = unit(i) * UNIT, live = at.live(t);
-        const size_t row = live ? (size_t)t * a.C : 0;
-        FetchG::ask(gpart, gate + row, a.C, live, a.C - at.c0);
-        FetchX::ask(xpart, x + row, a.C, live, a.C - at.c0);
+    auto ask = [&](int i, int place) {
+        if (i < hi - lo) {
+            const int t = unit(i) * UNIT, live = at.live(t);
+            const size_t row = live ? (size_t)t * a.C : 0;
+            FetchG::ask(part + place * bytes, gate + row, a.C, live, a.C - at.c0);
+            FetchX::ask(part + place * bytes + FetchG::BYTES, x + row, a.C, live, a.C - at.c0);
+        }
+        copies_end();
     };
     F<N> mg = all<N>(0.f), mb = mg;
     Marks marks;
-    if (V::STAGED && lo < hi) ask(0);
+    if (V::STAGED)
+        for (int i = 0; i < V::DEPTH; ++i) ask(i, i);
+    int place = 0;
     for (int i = 0; i < hi - lo; ++i) {
         const int t = unit(i) * UNIT, live = at.live(t);
         const size_t row = live ? (size_t)t * a.C : 0;
@@ -351,13 +325,14 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
         FetchG fg;
         FetchX fx;
         if (V::STAGED) {
-            copies_wait();
+            copies_wait<V::DEPTH - 1>();
             __syncwarp();
         }
-        fg.take(gpart, gate + row, a.C, live, at.c - at.c0, at.inside);
-        fx.take(xpart, x + row, a.C, live, at.c - at.c0, at.inside);
+        fg.take(part + place * bytes, gate + row, a.C, live, at.c - at.c0, at.inside);
+        fx.take(part + place * bytes + FetchG::BYTES, x + row, a.C, live, at.c - at.c0, at.inside);
         __syncwarp();
-        if (V::STAGED && i + 1 < hi - lo) ask(i + 1);
+        if (V::STAGED) ask(i + V::DEPTH, place);
+        place = place + 1 < V::DEPTH ? place + 1 : 0;
         int q = marks.s;
         if (FLAT && REVERSE)
             for (int k = 1; k < UNIT; ++k)
@@ -414,18 +389,17 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
 // Rows that are all there and begin and end no sequence take the code without tests.
 // out == nullptr: only the states are kept.
 template <typename V, bool COMP, bool FLAT, bool SPLIT>
-__global__ void __launch_bounds__(32 * V::WARPS, XFMIN / V::WARPS) scan_fwd_kernel(ScanArgs a)
+__global__ void __launch_bounds__(32 * V::WARPS) scan_fwd_kernel(ScanArgs a)
 {
     using T = typename V::T;
     using FetchG = Fetch<float, V>;
     using FetchX = Fetch<T, V>;
-    constexpr int N = V::VEC;
+    constexpr int N = V::VEC, PART = FetchG::BYTES + FetchX::BYTES;
     extern __shared__ __align__(16) char shared[];
     pdl_wait();
     const Stand<V, FLAT, SPLIT> at(a);
     Hand<V>& hand = *reinterpret_cast<Hand<V>*>(shared);
-    char* const gpart = shared + sizeof(Hand<V>) + at.warp * (FetchG::BYTES + FetchX::BYTES);
-    char* const xpart = gpart + FetchG::BYTES;
+    char* const part = shared + sizeof(Hand<V>) + at.warp * V::DEPTH * PART;
     const int c = at.c, l = (threadIdx.x & 31) * N;
     const T* x = static_cast<const T*>(a.x) + at.row0 * a.C + at.c0;
     const float* gate = a.gate + at.row0 * a.C + at.c0;
@@ -434,16 +408,20 @@ __global__ void __launch_bounds__(32 * V::WARPS, XFMIN / V::WARPS) scan_fwd_kern
     if (FLAT && a.cu && a.fin && at.inside) pass_empty<N>(a, a.init, a.fin, at.rank * V::WARPS + at.warp, a.span * V::WARPS, c);
     F<N> h = all<N>(0.f);
     if (!FLAT && at.inside) h = read_or_zero<N>(a.init, (size_t)at.s * a.C + c);
-    if (SPLIT) h = state_in_front<V, COMP, FLAT, false>(a, at, hand, h, gate, x, gpart, xpart);
-    auto ask = [&](int u) {
-        const int t = u * UNIT, live = at.live(t);
-        const size_t row = live ? (size_t)t * a.C : 0;
-        FetchG::ask(gpart, gate + row, a.C, live, a.C - at.c0);
-        FetchX::ask(xpart, x + row, a.C, live, a.C - at.c0);
+    if (SPLIT) h = state_in_front<V, COMP, FLAT, false>(a, at, hand, h, gate, x, part, PART);
+    auto ask = [&](int u, int place) {
+        if (u < at.last) {
+            const int t = u * UNIT, live = at.live(t);
+            const size_t row = live ? (size_t)t * a.C : 0;
+            FetchG::ask(part + place * PART, gate + row, a.C, live, a.C - at.c0);
+            FetchX::ask(part + place * PART + FetchG::BYTES, x + row, a.C, live, a.C - at.c0);
+        }
+        copies_end();
     };
     Marks marks;
-    int u = at.first + at.warp;
-    if (V::STAGED && u < at.last) ask(u);
+    int u = at.first + at.warp, place = 0;
+    if (V::STAGED)
+        for (int i = 0; i < V::DEPTH; ++i) ask(u + i * V::WARPS, i);
     for (; u < at.last; u += V::WARPS) {
         const int t = u * UNIT, live = at.live(t);
         const size_t row = (size_t)t * a.C;
@@ -452,13 +430,14 @@ __global__ void __launch_bounds__(32 * V::WARPS, XFMIN / V::WARPS) scan_fwd_kern
         FetchG fg;
         FetchX fx;
         if (V::STAGED) {
-            copies_wait();
+            copies_wait<V::DEPTH - 1>();
             __syncwarp();
         }
-        fg.take(gpart, gate + row, a.C, live, c - at.c0, at.inside);
-        fx.take(xpart, x + row, a.C, live, c - at.c0, at.inside);
+        fg.take(part + place * PART, gate + row, a.C, live, c - at.c0, at.inside);
+        fx.take(part + place * PART + FetchG::BYTES, x + row, a.C, live, c - at.c0, at.inside);
         __syncwarp();
-        if (V::STAGED && u + V::WARPS < at.last) ask(u + V::WARPS);
+        if (V::STAGED) ask(u + V::DEPTH * V::WARPS, place);
+        place = place + 1 < V::DEPTH ? place + 1 : 0;
         Decay<N> d[UNIT];
         F<N> b[UNIT];
         F<N> mg = all<N>(0.f), mb = mg;
@@ -483,15 +462,20 @@ __global__ void __launch_bounds__(32 * V::WARPS, XFMIN / V::WARPS) scan_fwd_kern
             mg = all<N>(-INFINITY);
         }
         const Decay<N> md = Decay<N>::of(mg);
-        if (u > at.first) {
-            take_over(at.warp);
-            h = read<N>(&hand.state[at.warp][l]);
-        }
-        const F<N> behind = md.step(h, mb);
-        if (u + 1 < at.last) {
-            const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
-            write<N>(&hand.state[next][l], behind);
-            hand_on(next);
+        F<N> behind;
+        const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
+        if (u > at.first && u + 1 < at.last) {
+            h = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
+        } else {
+            if (u > at.first) {
+                take_over(at.warp);
+                h = read<N>(&hand.state[at.warp][l]);
+            }
+            behind = md.step(h, mb);
+            if (u + 1 < at.last) {
+                write<N>(&hand.state[next][l], behind);
+                hand_on(next);
+            }
         }
         if (!FLAT && a.fin && u + 1 == a.units && at.inside) write<N>(a.fin + (size_t)at.s * a.C + c, behind);
         if (plain) {
@@ -524,7 +508,7 @@ __global__ void __launch_bounds__(32 * V::WARPS, XFMIN / V::WARPS) scan_fwd_kern
 // forward again from the one that the forward kept, so that the gates' gradients take fp32 states:
 //   dgate_t = (h_{t-1} [- x_t]) e_t,   dx_t = dh_t or (1 - a_t) dh_t,   dh_t = dout_t + e_{t+1}.
 template <typename V, bool COMP, bool FLAT, bool SPLIT>
-__global__ void __launch_bounds__(32 * V::WARPS, XBMIN / V::WARPS) scan_bwd_kernel(ScanArgs a)
+__global__ void __launch_bounds__(32 * V::WARPS) scan_bwd_kernel(ScanArgs a)
 {
     using T = typename V::T;
     using FetchG = Fetch<float, V>;
@@ -534,9 +518,7 @@ __global__ void __launch_bounds__(32 * V::WARPS, XBMIN / V::WARPS) scan_bwd_kern
     pdl_wait();
     const Stand<V, FLAT, SPLIT> at(a);
     Hand<V>& hand = *reinterpret_cast<Hand<V>*>(shared);
-    char* const gpart = shared + sizeof(Hand<V>) + at.warp * PART;
-    char* const xpart = gpart + FetchG::BYTES;
-    char* const ypart = xpart + FetchX::BYTES;
+    char* const part = shared + sizeof(Hand<V>) + at.warp * V::DEPTH * PART;
     const int c = at.c, l = (threadIdx.x & 31) * N;
     const T* x = static_cast<const T*>(a.x) + at.row0 * a.C + at.c0;
     const T* dout = static_cast<const T*>(a.dout) + at.row0 * a.C + at.c0;
@@ -547,17 +529,22 @@ __global__ void __launch_bounds__(32 * V::WARPS, XBMIN / V::WARPS) scan_bwd_kern
     if (FLAT && a.cu && a.dinit && at.inside) pass_empty<N>(a, a.dfin, a.dinit, at.rank * V::WARPS + at.warp, a.span * V::WARPS, c);
     F<N> e = all<N>(0.f);
     if (!FLAT && at.inside) e = read_or_zero<N>(a.dfin, (size_t)at.s * a.C + c);
-    if (SPLIT) e = state_in_front<V, COMP, FLAT, true>(a, at, hand, e, gate, dout, gpart, ypart);
-    auto ask = [&](int u) {
-        const int t = u * UNIT, live = at.live(t);
-        const size_t row = live ? (size_t)t * a.C : 0;
-        FetchG::ask(gpart, gate + row, a.C, live, a.C - at.c0);
-        FetchX::ask(xpart, x + row, a.C, live, a.C - at.c0);
-        FetchX::ask(ypart, dout + row, a.C, live, a.C - at.c0);
+    if (SPLIT) e = state_in_front<V, COMP, FLAT, true>(a, at, hand, e, gate, dout, part, PART);
+    auto ask = [&](int u, int place) {
+        if (u >= at.first) {
+            const int t = u * UNIT, live = at.live(t);
+            const size_t row = live ? (size_t)t * a.C : 0;
+            char* const to = part + place * PART;
+            FetchG::ask(to, gate + row, a.C, live, a.C - at.c0);
+            FetchX::ask(to + FetchG::BYTES, x + row, a.C, live, a.C - at.c0);
+            FetchX::ask(to + FetchG::BYTES + FetchX::BYTES, dout + row, a.C, live, a.C - at.c0);
+        }
+        copies_end();
     };
     Marks marks;
-    int u = at.last - 1 - at.warp;
-    if (V::STAGED && u >= at.first) ask(u);
+    int u = at.last - 1 - at.warp, place = 0;
+    if (V::STAGED)
+        for (int i = 0; i < V::DEPTH; ++i) ask(u - i * V::WARPS, i);
     for (; u >= at.first; u -= V::WARPS) {
         const int t = u * UNIT, live = at.live(t);
         const size_t row = (size_t)t * a.C;
@@ -568,14 +555,16 @@ __global__ void __launch_bounds__(32 * V::WARPS, XBMIN / V::WARPS) scan_bwd_kern
         FetchG fg;
         FetchX fx, fy;
         if (V::STAGED) {
-            copies_wait();
+            copies_wait<V::DEPTH - 1>();
             __syncwarp();
         }
-        fg.take(gpart, gate + row, a.C, live, c - at.c0, at.inside);
-        fx.take(xpart, x + row, a.C, live, c - at.c0, at.inside);
-        fy.take(ypart, dout + row, a.C, live, c - at.c0, at.inside);
+        const char* const from = part + place * PART;
+        fg.take(from, gate + row, a.C, live, c - at.c0, at.inside);
+        fx.take(from + FetchG::BYTES, x + row, a.C, live, c - at.c0, at.inside);
+        fy.take(from + FetchG::BYTES + FetchX::BYTES, dout + row, a.C, live, c - at.c0, at.inside);
         __syncwarp();
-        if (V::STAGED && u - V::WARPS >= at.first) ask(u - V::WARPS);
+        if (V::STAGED) ask(u - V::DEPTH * V::WARPS, place);
+        place = place + 1 < V::DEPTH ? place + 1 : 0;
         Decay<N> d[UNIT];
         F<N> before[UNIT];
         F<N> mg = all<N>(0.f), mb = mg;
@@ -603,15 +592,20 @@ __global__ void __launch_bounds__(32 * V::WARPS, XBMIN / V::WARPS) scan_bwd_kern
             if (FLAT && i && (marks.first >> i & 1)) q = previous(a, q);
         }
         const Decay<N> md = Decay<N>::of(mg);
-        if (u + 1 < at.last) {
-            take_over(at.warp);
-            e = read<N>(&hand.state[at.warp][l]);
-        }
-        const F<N> behind = md.step(e, mb);
-        if (u > at.first) {
-            const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
-            write<N>(&hand.state[next][l], behind);
-            hand_on(next);
+        F<N> behind;
+        const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
+        if (u > at.first && u + 1 < at.last) {
+            e = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
+        } else {
+            if (u + 1 < at.last) {
+                take_over(at.warp);
+                e = read<N>(&hand.state[at.warp][l]);
+            }
+            behind = md.step(e, mb);
+            if (u > at.first) {
+                write<N>(&hand.state[next][l], behind);
+                hand_on(next);
+            }
         }
         if (!FLAT && a.dinit && u == 0 && at.inside) write<N>(a.dinit + (size_t)at.s * a.C + c, behind);
         if (plain) {
@@ -683,14 +677,34 @@ ScanArgs make_args(const osdn_scan_params& p)
     return a;
 }
 
-// Kernel(SPLIT) for the walks of a batch.  A walk is split until there is a CTA for each SM: its CTAs read their rows twice.
+// CTAs of a walk.  One, where walks alone give four of five SMs a CTA; else the walk is split, though its CTAs then read their
+// rows twice, until there are CTAs for all SMs, as long as every warp has eight units (one prompt of 2048 tokens, 1024 channels,
+// forward: 13.8 us with eight CTAs to a walk, 16.3 with sixteen; 131072 tokens 614 and 551).
+int span_of(long long walks, int units, int warps)
+{
+    int span = 1;
+    if (walks < 120)
+        while (span < MAX_SPAN && units >= 8 * span * warps && walks * span < 240) span *= 2;
+    return span;
+}
+
+// Warps of a CTA.  Sixteen where an SM has one CTA with enough units for them, eight where it has two or the walk is short
+// (forward, 1024 channels, sixteen and eight: 8 x 2048 tokens 28.7 and 29.4 us, backward 40.9 and 52.1; 32 x 2048 106 and
+// 97; 64 x 100 23.5 and 15.4; one of 2048 22.0 and 15.7).
+int warps_of(const ScanArgs& a, bool flat, int channels)
+{
+    const long long walks = (long long)(flat ? 1 : a.S) * div_up(a.C, channels);
+    const int span = span_of(walks, a.units, 16);
+    return walks < 240 && a.units / span >= (span > 1 ? 256 : 64) ? 16 : 8;
+}
+
+// Kernel(SPLIT) for the walks of a batch.
 template <typename V, typename K> bool launch_walks(K kernel, ScanArgs a, bool flat, int part, cudaStream_t st)
 {
     const long long walks = (long long)(flat ? 1 : a.S) * div_up(a.C, V::CB);
-    a.span = 1;
-    while (a.span < MAX_SPAN && a.units >= 2 * a.span * V::WARPS && walks * a.span < XCTA) a.span *= 2;
+    a.span = span_of(walks, a.units, V::WARPS);
     const bool split = a.span > 1;
-    const size_t smem = sizeof(Hand<V>) + (V::STAGED ? (size_t)V::WARPS * part : 0);
+    const size_t smem = sizeof(Hand<V>) + (V::STAGED ? (size_t)V::WARPS * V::DEPTH * part : 0);
     void (*f)(ScanArgs) = split ? kernel(std::true_type{}) : kernel(std::false_type{});
     if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
     if (a.span > 8 && cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
@@ -722,7 +736,8 @@ template <typename T, bool COMP> bool launch_forward(const ScanArgs& a, bool fla
         };
         return launch_walks<V>(kernel, a, flat, Fetch<float, V>::BYTES + Fetch<T, V>::BYTES, st);
     };
-    return is_wide<T>(a.C) ? go(Cover<T, 2, XW>{}) : go(Cover<T, 1, XW>{});
+    if (!is_wide<T>(a.C)) return go(Cover<T, 1, 8, 1>{});
+    return warps_of(a, flat, 64) == 16 ? go(Cover<T, 2, 16, 1>{}) : go(Cover<T, 2, 8, 2>{});
 }
 
 template <typename T, bool COMP> int run_backward(const ScanArgs& a, bool flat, bool saved, cudaStream_t st)
@@ -740,7 +755,10 @@ template <typename T, bool COMP> int run_backward(const ScanArgs& a, bool flat, 
         };
         return launch_walks<V>(kernel, a, flat, Fetch<float, V>::BYTES + 2 * Fetch<T, V>::BYTES, st);
     };
-    return (is_wide<T>(a.C) ? go(Cover<T, 2, XW>{}) : go(Cover<T, 1, XW>{})) ? n : -1;
+    const bool ok = !is_wide<T>(a.C)               ? go(Cover<T, 1, 8, 1>{})
+                    : warps_of(a, flat, 64) == 16 ? go(Cover<T, 2, 16, 2>{})
+                                                  : go(Cover<T, 2, 8, 2>{});
+    return ok ? n : -1;
 }
 
 template <typename T, int N, bool COMP>
