@@ -223,6 +223,15 @@ template <typename T, int N> struct Channels {
     }
 };
 
+__device__ __forceinline__ void copy_async16(void* smem, const void* src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(src),
+                 "r"(real ? 16 : 0) : "memory");   // what is not there is filled with zeros
+}
+// Stretches of rows come in through several places of shared memory: one group of copies for each, empty ones too.
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LATER> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory"); }
+
 inline int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // Entry points of the kernels' files.  The number of launches, or -1 on a launch error.

@@ -98,15 +98,6 @@ template <int N> __device__ __forceinline__ void write(__nv_bfloat16* p, const F
     else *p = __float2bfloat16_rn(a.x[0]);
 }
 
-__device__ __forceinline__ void copy_async16(void* smem, const void* src, bool real)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(src),
-                 "r"(real ? 16 : 0) : "memory");   // what is not there is filled with zeros
-}
-// A warp's units come in through DEPTH places of shared memory: one group of copies a unit, empty ones too.
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LATER> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory"); }
-
 // A warp's TPG rows of one tensor.  Staged: the warp copies them in 16-byte pieces to its own part of shared memory.
 template <typename E, typename V> struct Fetch {
     Raw<E, V::VEC> r[V::TPG];
