@@ -322,7 +322,7 @@ typedef struct osdn_scan_params {
 } osdn_scan_params;
 
 /* Bytes of the workspace that connects a forward that saves residuals with its backward (the states at
- * every 128th token, fp32); 0 on invalid params. */
+ * every eighth token, fp32); 0 on invalid params. */
 size_t osdn_scan_workspace_bytes(const osdn_scan_params* p);
 
 /*

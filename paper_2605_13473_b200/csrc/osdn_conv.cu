@@ -441,7 +441,7 @@ template <typename F> int by_type(const osdn_conv_params& p, F f)   // f(element
 }
 
 // Rows of a walk (a multiple of eight): as many as let the walks of 128 rows at most fill every SM's `ctas` CTAs a whole number
-// of times.  (8 x 2048 x 2048 in walks of 64 rows, 1.15 times: forward 28.9 us, in walks of 80 XX.)
+// of times.  (8 x 2048 x 2048 in walks of 64 rows, 1.15 times: forward 28.9 us, in walks of 80 26.9.)
 void plan_walks(ConvArgs& a, const osdn_conv_params& p, int N, int ctas)
 {
     const long long blocks = div_up(p.C, 32 * N), rows = (long long)p.B * p.T * blocks, slots = 148ll * ctas;

@@ -6,35 +6,56 @@
 namespace osdn {
 namespace {
 
-constexpr int UNIT = 8;   // rows that a warp takes at a time; the forward keeps the state in front of each such stretch for the backward
+constexpr int SIDE = 4;   // rows whose factors are worked out side by side (one by one: forward of 8 x 2048 tokens 36 us, so 27)
+// Rows that a warp takes at a time; the forward keeps the state in front of each such stretch for the backward.
+constexpr int UNIT = 8;
 
 // exp(g) for g <= 0 as the sum of two floats, hi the nearest one to it:
 //   |g| <= 1/4:  from expm1(g) by its Taylor series to g^6 (remainder below 5e-8 of it): the sum keeps the distance from one;
 //   else:        hi alone, by the hardware's exponential (2^-22 of a; a <= 0.78 forgets it within a few tokens); -inf is zero.
 // As one rounded factor, a gate of -3e-4 keeps 1 - a to 1e-4 only, and a product of thousands of them drifts.  Two floats cost
-// one packed fma more a step and no selection (with the form chosen at every step: 38 instructions an element against 22).
+// one packed fma more a step and no selection (with the form chosen at every step 38 instructions an element instead of 29).
 template <int N> struct Decay {
     F<N> hi, lo;
     __device__ __forceinline__ static Decay of(const F<N>& g)
     {
-        F<N> q = fma(g, all<N>(1.f / 720), all<N>(1.f / 120));
-        q = fma(g, q, all<N>(1.f / 24));
-        q = fma(g, q, all<N>(1.f / 6));
-        q = fma(g, q, all<N>(0.5f));
-        const F<N> p = fma(mul(g, g), q, g);
-        const F<N> e = mul(g, all<N>(1.44269504f));
-        const F<N> near = add(p, all<N>(1.f));
-        const F<N> rest = add(p, fma(near, all<N>(-1.f), all<N>(1.f)));   // p - (near - 1), exact
-        Decay d;
+        Decay d[1];
+        of<1>(&g, d);
+        return d[0];
+    }
+    // K of them step by step side by side: one alone is a chain of ten dependent operations
+    template <int K> __device__ __forceinline__ static void of(const F<N>* g, Decay* d)
+    {
+        F<N> q[K];
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            float w;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(e.x[k]));
-            const bool is = fabsf(g.x[k]) <= 0.25f;
-            d.hi.x[k] = is ? near.x[k] : w;
-            d.lo.x[k] = is ? rest.x[k] : 0.f;
+        for (int i = 0; i < K; ++i) q[i] = mul(g[i], all<N>(1.44269504f));
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+#pragma unroll
+            for (int k = 0; k < N; ++k) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d[i].hi.x[k]) : "f"(q[i].x[k]));
+#pragma unroll
+        for (int i = 0; i < K; ++i) q[i] = fma(g[i], all<N>(1.f / 720), all<N>(1.f / 120));
+#pragma unroll
+        for (int i = 0; i < K; ++i) q[i] = fma(g[i], q[i], all<N>(1.f / 24));
+#pragma unroll
+        for (int i = 0; i < K; ++i) q[i] = fma(g[i], q[i], all<N>(1.f / 6));
+#pragma unroll
+        for (int i = 0; i < K; ++i) q[i] = fma(g[i], q[i], all<N>(0.5f));
+#pragma unroll
+        for (int i = 0; i < K; ++i) q[i] = mul(g[i], q[i]);
+#pragma unroll
+        for (int i = 0; i < K; ++i) q[i] = fma(g[i], q[i], g[i]);
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const F<N> near = add(q[i], all<N>(1.f));
+            const F<N> rest = add(q[i], fma(near, all<N>(-1.f), all<N>(1.f)));   // p - (near - 1), exact
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const bool is = fabsf(g[i].x[k]) <= 0.25f;
+                d[i].hi.x[k] = is ? near.x[k] : d[i].hi.x[k];
+                d[i].lo.x[k] = is ? rest.x[k] : 0.f;
+            }
         }
-        return d;
     }
     __device__ __forceinline__ F<N> complement() const { return fma(lo, all<N>(-1.f), fma(hi, all<N>(-1.f), all<N>(1.f))); }   // 1 - a
     __device__ __forceinline__ F<N> times(const F<N>& y) const { return fma(hi, y, mul(lo, y)); }                    // a y
@@ -107,13 +128,19 @@ template <typename E, typename V> struct Fetch {
     {
         if constexpr (V::STAGED) {
             constexpr int PIECES = ROW / 16, ROWS = 32 / PIECES, PER = 16 / (int)sizeof(E);
-            const int lane = threadIdx.x & 31, row = lane / PIECES, col = (lane % PIECES) * PER;
-            const bool in = col < cols;
-            const E* from = p + (in ? row * pitch + col : 0);
+            const int lane = threadIdx.x & 31, row = lane / PIECES;
+            const int col = (lane % PIECES) * PER;
+            char* const to = part + lane * 16;
+            const E* from = p + row * pitch + col;
+            if (live >= V::TPG && cols >= V::CB) {   // nearly always
 #pragma unroll
-            for (int i = 0; i < V::TPG; i += ROWS) {
-                const bool real = in && i + row < live;
-                copy_async16(part + i * ROW + lane * 16, real ? from + i * pitch : p, real);
+                for (int i = 0; i < V::TPG; i += ROWS, from += ROWS * pitch) copy_async16(to + i * ROW, from, true);
+                return;
+            }
+#pragma unroll
+            for (int i = 0; i < V::TPG; i += ROWS, from += ROWS * pitch) {
+                const bool real = col < cols && i + row < live;
+                copy_async16(to + i * ROW, real ? from : p, real);
             }
         }
     }
@@ -237,6 +264,15 @@ __device__ __forceinline__ F<N> relay(int id, int next_id, const float* mine, fl
     }
 }
 
+// What the second walk over a unit needs is worked out before the wait for the state, and not put off or done again behind it.
+template <int N> __device__ __forceinline__ void pin(Decay<N> (&d)[UNIT], F<N> (&y)[UNIT])
+{
+#pragma unroll
+    for (int i = 0; i < UNIT; ++i)
+#pragma unroll
+        for (int k = 0; k < N; ++k) asm volatile("" : "+f"(d[i].hi.x[k]), "+f"(d[i].lo.x[k]), "+f"(y[i].x[k]));
+}
+
 // The sequence in front of q that is not empty (one there is: q does not begin the rows).
 __device__ __forceinline__ int previous(const ScanArgs& a, int q)
 {
@@ -324,27 +360,44 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
         __syncwarp();
         if (V::STAGED) ask(i + V::DEPTH, place);
         place = place + 1 < V::DEPTH ? place + 1 : 0;
-        int q = marks.s;
-        if (FLAT && REVERSE)
-            for (int k = 1; k < UNIT; ++k)
-                if (marks.first >> k & 1) q = Marks::next(a, q, t + k);
+        if (!FLAT || !(REVERSE ? marks.last : marks.first)) {
+            Decay<N> d[UNIT];
+            F<N> b[UNIT];
 #pragma unroll
-        for (int k = 0; k < UNIT; ++k) {
-            const int j = REVERSE ? UNIT - 1 - k : k;
-            const F<N> g = fg.r[j].get(), y = fx.r[j].get();
-            const Decay<N> d = Decay<N>::of(g);
-            if (FLAT && !REVERSE && (marks.first >> j & 1)) {
-                if (j) q = Marks::next(a, q, t + j);
-                mb = at.inside ? read_or_zero<N>(a.init, (size_t)q * a.C + at.c) : all<N>(0.f);
-                mg = all<N>(-INFINITY);
+            for (int j = 0; j < UNIT; j += SIDE) {
+                F<N> g[SIDE];
+#pragma unroll
+                for (int i = 0; i < SIDE; ++i) {
+                    g[i] = fg.r[j + i].get();
+                    mg = add(mg, g[i]);
+                }
+                Decay<N>::template of<SIDE>(g, d + j);
+#pragma unroll
+                for (int i = j; i < j + SIDE; ++i) b[i] = COMP && !REVERSE ? mul(d[i].complement(), fx.r[i].get()) : fx.r[i].get();
             }
-            if (FLAT && REVERSE && (marks.last >> j & 1)) {
-                mb = at.inside ? read_or_zero<N>(a.dfin, (size_t)q * a.C + at.c) : all<N>(0.f);
-                mg = all<N>(-INFINITY);
+#pragma unroll
+            for (int k = 0; k < UNIT; ++k) {
+                const int j = REVERSE ? UNIT - 1 - k : k;
+                mb = REVERSE ? d[j].times(add(b[j], mb)) : d[j].step(mb, b[j]);
             }
-            mg = add(mg, g);
-            mb = REVERSE ? d.times(add(y, mb)) : d.step(mb, COMP ? mul(d.complement(), y) : y);
-            if (FLAT && REVERSE && j && (marks.first >> j & 1)) q = previous(a, q);
+        } else {
+            int q = marks.s;
+            if (REVERSE)
+                for (int k = 1; k < UNIT; ++k)
+                    if (marks.first >> k & 1) q = Marks::next(a, q, t + k);
+#pragma unroll
+            for (int k = 0; k < UNIT; ++k) {
+                const int j = REVERSE ? UNIT - 1 - k : k;
+                const F<N> y = fx.r[j].get();
+                const Decay<N> d = Decay<N>::of(fg.r[j].get());
+                if ((REVERSE ? marks.last : marks.first) >> j & 1) {
+                    if (!REVERSE && j) q = Marks::next(a, q, t + j);
+                    mb = at.inside ? read_or_zero<N>(REVERSE ? a.dfin : a.init, (size_t)q * a.C + at.c) : all<N>(0.f);
+                }
+                mb = REVERSE ? d.times(add(y, mb)) : d.step(mb, COMP ? mul(d.complement(), y) : y);
+                if (REVERSE && j && (marks.first >> j & 1)) q = previous(a, q);
+            }
+            mg = all<N>(-INFINITY);
         }
     }
     write<N>(&hand.g[at.warp][l], mg);
@@ -374,13 +427,15 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
 // One walk = one dense sequence, or a whole flat batch with resets where sequences begin, over CB channels.  A CTA's warps take
 // units of UNIT rows in turn: a warp maps its rows to (sum of gates, b), waits for the state in front of them, hands the
 // state behind them on to the next warp before it does anything else, and walks the rows a second time from registers.  So
-// the only thing done one after another is a step of two fmas a unit (about 100 cycles from warp to warp by named barriers);
-// with barriers of all warps instead, tile by tile, the warps waited more than they worked (38 to 51 us against XX).
+// the only thing done one after another is a step of two fmas a unit, from warp to warp by named barriers.  With barriers of
+// all warps instead, tile by tile, the warps waited more than they worked (8 x 2048 tokens, 1024 channels, bf16: 38 to 51 us;
+// so 27.3, 4.9 TB/s of what has to be read and written, and the backward 41.5, 5.7 TB/s).  29 instructions an element, of which
+// the factor takes nine; bound by their issue and latency in bf16, by memory in fp32 (5.9 TB/s).
 // Few walks are split among the CTAs of a cluster, which read their rows once more for the state in front of them.
 // Rows that are all there and begin and end no sequence take the code without tests.
 // out == nullptr: only the states are kept.
 template <typename V, bool COMP, bool FLAT, bool SPLIT>
-__global__ void __launch_bounds__(32 * V::WARPS) scan_fwd_kernel(ScanArgs a)
+__global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_fwd_kernel(ScanArgs a)
 {
     using T = typename V::T;
     using FetchG = Fetch<float, V>;
@@ -433,12 +488,18 @@ __global__ void __launch_bounds__(32 * V::WARPS) scan_fwd_kernel(ScanArgs a)
         F<N> b[UNIT];
         F<N> mg = all<N>(0.f), mb = mg;
 #pragma unroll
-        for (int i = 0; i < UNIT; ++i) {
-            const F<N> g = fg.r[i].get(), y = fx.r[i].get();
-            d[i] = Decay<N>::of(g);
-            b[i] = COMP ? mul(d[i].complement(), y) : y;
-            mg = add(mg, g);
-            mb = d[i].step(mb, b[i]);
+        for (int j = 0; j < UNIT; j += SIDE) {
+            F<N> g[SIDE];
+#pragma unroll
+            for (int i = 0; i < SIDE; ++i) {
+                g[i] = fg.r[j + i].get();
+                mg = add(mg, g[i]);
+            }
+            Decay<N>::template of<SIDE>(g, d + j);
+#pragma unroll
+            for (int i = j; i < j + SIDE; ++i) b[i] = COMP ? mul(d[i].complement(), fx.r[i].get()) : fx.r[i].get();
+#pragma unroll
+            for (int i = j; i < j + SIDE; ++i) mb = d[i].step(mb, b[i]);
         }
         if (FLAT && marks.first) {
             int q = marks.s;
@@ -454,6 +515,7 @@ __global__ void __launch_bounds__(32 * V::WARPS) scan_fwd_kernel(ScanArgs a)
         }
         const Decay<N> md = Decay<N>::of(mg);
         F<N> behind;
+        pin<N>(d, b);
         const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
         if (u > at.first && u + 1 < at.last) {
             h = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
@@ -499,7 +561,7 @@ __global__ void __launch_bounds__(32 * V::WARPS) scan_fwd_kernel(ScanArgs a)
 // forward again from the one that the forward kept, so that the gates' gradients take fp32 states:
 //   dgate_t = (h_{t-1} [- x_t]) e_t,   dx_t = dh_t or (1 - a_t) dh_t,   dh_t = dout_t + e_{t+1}.
 template <typename V, bool COMP, bool FLAT, bool SPLIT>
-__global__ void __launch_bounds__(32 * V::WARPS) scan_bwd_kernel(ScanArgs a)
+__global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_bwd_kernel(ScanArgs a)
 {
     using T = typename V::T;
     using FetchG = Fetch<float, V>;
@@ -559,31 +621,52 @@ __global__ void __launch_bounds__(32 * V::WARPS) scan_bwd_kernel(ScanArgs a)
         Decay<N> d[UNIT];
         F<N> before[UNIT];
         F<N> mg = all<N>(0.f), mb = mg;
-        int q = marks.s;
 #pragma unroll
-        for (int i = 0; i < UNIT; ++i) {
-            const F<N> g = fg.r[i].get(), y = fx.r[i].get();
-            d[i] = Decay<N>::of(g);
-            mg = add(mg, g);
-            if (FLAT && (marks.first >> i & 1)) {
-                if (i) q = Marks::next(a, q, t + i);
-                h = at.inside ? read_or_zero<N>(a.init, (size_t)q * a.C + c) : all<N>(0.f);
+        for (int j = 0; j < UNIT; j += SIDE) {
+            F<N> g[SIDE];
+#pragma unroll
+            for (int i = 0; i < SIDE; ++i) {
+                g[i] = fg.r[j + i].get();
+                mg = add(mg, g[i]);
             }
-            before[i] = h;
-            h = d[i].step(h, COMP ? mul(d[i].complement(), y) : y);
+            Decay<N>::template of<SIDE>(g, d + j);
         }
-        const int qlast = q;   // against time: the sequence of the last row first
+        int qlast = 0;   // against time: the sequence of the last row first
+        if (!FLAT || !(marks.first | marks.last)) {
 #pragma unroll
-        for (int i = UNIT - 1; i >= 0; --i) {
-            if (FLAT && (marks.last >> i & 1)) {
-                mb = at.inside ? read_or_zero<N>(a.dfin, (size_t)q * a.C + c) : all<N>(0.f);
-                mg = all<N>(-INFINITY);
+            for (int i = 0; i < UNIT; ++i) {
+                const F<N> y = fx.r[i].get();
+                before[i] = h;
+                h = d[i].step(h, COMP ? mul(d[i].complement(), y) : y);
             }
-            mb = d[i].times(add(fy.r[i].get(), mb));
-            if (FLAT && i && (marks.first >> i & 1)) q = previous(a, q);
+#pragma unroll
+            for (int i = UNIT - 1; i >= 0; --i) mb = d[i].times(add(fy.r[i].get(), mb));
+        } else {
+            int q = marks.s;
+#pragma unroll
+            for (int i = 0; i < UNIT; ++i) {
+                if (marks.first >> i & 1) {
+                    if (i) q = Marks::next(a, q, t + i);
+                    h = at.inside ? read_or_zero<N>(a.init, (size_t)q * a.C + c) : all<N>(0.f);
+                }
+                const F<N> y = fx.r[i].get();
+                before[i] = h;
+                h = d[i].step(h, COMP ? mul(d[i].complement(), y) : y);
+            }
+            qlast = q;
+#pragma unroll
+            for (int i = UNIT - 1; i >= 0; --i) {
+                if (marks.last >> i & 1) {
+                    mb = at.inside ? read_or_zero<N>(a.dfin, (size_t)q * a.C + c) : all<N>(0.f);
+                    mg = all<N>(-INFINITY);
+                }
+                mb = d[i].times(add(fy.r[i].get(), mb));
+                if (i && (marks.first >> i & 1)) q = previous(a, q);
+            }
         }
         const Decay<N> md = Decay<N>::of(mg);
         F<N> behind;
+        pin<N>(d, before);
         const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
         if (u > at.first && u + 1 < at.last) {
             e = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
@@ -608,7 +691,7 @@ __global__ void __launch_bounds__(32 * V::WARPS) scan_bwd_kernel(ScanArgs a)
                 write<N>(dgate + row + (size_t)i * a.C, mul(COMP ? fma(fx.r[i].get(), all<N>(-1.f), before[i]) : before[i], e));
             }
         } else if (at.inside) {
-            q = qlast;
+            int q = qlast;
 #pragma unroll
             for (int i = UNIT - 1; i >= 0; --i) {
                 if (i >= live) continue;
@@ -669,13 +752,13 @@ ScanArgs make_args(const osdn_scan_params& p)
 }
 
 // CTAs of a walk.  One, where walks alone give four of five SMs a CTA; else the walk is split, though its CTAs then read their
-// rows twice, until there are CTAs for all SMs, as long as every warp has eight units (one prompt of 2048 tokens, 1024 channels,
-// forward: 13.8 us with eight CTAs to a walk, 16.3 with sixteen; 131072 tokens 614 and 551).
+// rows twice, until there are CTAs for four of five SMs, or for all of them twice over where every warp has many units (one
+// prompt of 2048 tokens, 1024 channels, forward: 13.8 us with eight CTAs to a walk, 16.3 with sixteen; 131072 tokens 614 and 551).
 int span_of(long long walks, int units, int warps)
 {
     int span = 1;
     if (walks < 120)
-        while (span < MAX_SPAN && units >= 8 * span * warps && walks * span < 240) span *= 2;
+        while (span < MAX_SPAN && units >= 2 * span * warps && walks * span < (units >= 64 * span * warps ? 240 : 120)) span *= 2;
     return span;
 }
 

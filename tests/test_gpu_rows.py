@@ -534,3 +534,103 @@ def test_a_block_from_projection_to_layer_and_its_decode():
         osdn.osdn_scan_step(osdn.make_scan_params(**one, C=H * D, input_gate="complement"), v, rgate[:, t].contiguous(), r, ht)
         assert torch.allclose(ot, out[:, t], atol=1e-5, rtol=1e-4) and torch.allclose(ht, h[:, t], atol=1e-5, rtol=1e-5)
     assert torch.allclose(S, S_all, atol=1e-5, rtol=1e-4) and torch.allclose(r, r_all, atol=1e-5, rtol=1e-5)
+
+
+@pytest.mark.parametrize("io", ["bf16", "fp32"])
+@pytest.mark.parametrize("B,T", [(130, 523), (131, 70), (300, 200), (1300, 9)])
+def test_scan_of_many_sequences(io, B, T):
+    """More walks than SMs, with few and with many rows: copies of one sequence give copies of its result."""
+    C = 64
+    x, gate = _scan_inputs(T, C, io, B + T)
+    g = _gen(B)
+    init, dfin, dout = torch.randn(1, C, generator=g), torch.randn(1, C, generator=g), torch.randn(T, C, generator=g).to(DT[io])
+    many = lambda t: t.repeat(B, 1)  # noqa: E731
+    got = _run_scan(many(x), many(gate), [T] * B, True, C, io, True, many(init), many(dout), many(dfin))
+    for name, a, b in zip(("out", "final", "dx", "dgate", "dinit"), got, ref.scan(x, gate, [T], init, True, dout, dfin)):
+        ref.check(a.view(B, -1, C)[0].contiguous(), b, name)
+        ref.check(a.view(B, -1, C)[B - 1].contiguous(), b, name)
+        if T >= 64:    # short sequences share units, at places of their own
+            assert bool((a.view(B, -1, C) == a.view(B, -1, C)[:1]).all()), name
+
+
+@pytest.mark.parametrize("lens", [[40000], [25000, 1, 0, 6, 14993]])
+def test_scan_of_one_long_row_split_over_a_cluster(lens):
+    C, N = 64, sum(lens)
+    x, gate = _scan_inputs(N, C, "bf16", 77)
+    g = _gen(78)
+    init, dfin = torch.randn(len(lens), C, generator=g), torch.randn(len(lens), C, generator=g)
+    dout = torch.randn(N, C, generator=g).to(torch.bfloat16)
+    got = _run_scan(x, gate, lens, len(lens) == 1, C, "bf16", False, init, dout, dfin)
+    for name, a, b in zip(("out", "final", "dx", "dgate", "dinit"), got, ref.scan(x, gate, lens, init, False, dout, dfin)):
+        ref.check(a, b, name)
+
+
+@pytest.mark.parametrize("T,Hq,Hk,D", [(9500, 3, 2, 64), (5000, 1, 1, 128), (2500, 5, 1, 256)])
+def test_norm_of_many_tokens_behind_a_padded_end(T, Hq, Hk, D):
+    """Whole tokens to a lane group, heads of odd numbers, the last sequence's end inside the rows."""
+    live = T - 333
+    g = _gen(T)
+    q, k = torch.randn(T, Hq, D, generator=g), torch.randn(T, Hk, D, generator=g)
+    q[live:], k[live:] = float("nan"), float("nan")
+    w = 1.0 + 0.2 * torch.randn(D, generator=g)
+    inv = 10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64) / D)
+    cu = _cu([1000, 0, live - 1000])
+    places = torch.cat([torch.arange(1000), torch.arange(live - 1000)])
+    d = lambda t: t.to(DEV)  # noqa: E731
+    for layout in ("half", "pairs"):
+        p = osdn.make_qk_norm_params(B=1, T=T, Hq=Hq, Hk=Hk, D=D, io_dtype="fp32", norm="rms", rot_dim=D, rot_layout=layout, cu_seqlens=cu)
+        y = [torch.full_like(t, MARK, device=DEV) for t in (q, k, q, k)]
+        dw = [torch.empty(D, device=DEV) for _ in range(2)]
+        osdn.osdn_qk_norm_fwd(p, d(q), d(k), d(w), None, d(inv), None, y[0], y[1])
+        osdn.osdn_qk_norm_bwd(p, d(q), d(k), d(w), None, d(inv), None, d(q), d(k), y[2], y[3], dw[0], None,
+                              torch.empty(osdn.osdn_qk_norm_workspace_bytes(p), device=DEV, dtype=torch.uint8))
+        angle = ref.angles(places, inv)
+        for t, wt, a, b, s in ((q, w, y[0], y[2], dw[0]), (k, None, y[1], y[3], None)):
+            want = ref.norm(t[:live], wt, "rms", 1e-6, angle, layout, t[:live])
+            ref.check(a[:live], want[0], "y")
+            ref.check(b[:live], want[1], "dx")
+            if s is not None:
+                ref.check(s, want[2], "dw")
+        for a in y:
+            assert bool((a[live:] == MARK).all())
+
+
+@pytest.mark.parametrize("broken", [[0, 300, 100, 500], [0, 600, 600, 900], [-50, 100, 200, 400], [700, 20, 10, -3], [0, 0, 0, 0]])
+def test_broken_boundaries_stay_inside_the_tensors(broken):
+    """What comes out is undefined; what lies around the tensors is not touched and every call ends."""
+    N, C, guard = 500, 64, 64
+    cu = torch.tensor(broken, dtype=torch.int32, device=DEV)
+
+    def inside(*shape, dt=torch.float32):
+        n = 1
+        for s in shape:
+            n *= s
+        whole = torch.full((n + 2 * guard,), MARK, device=DEV, dtype=dt)
+        return whole, whole[guard:guard + n].view(*shape)
+
+    bufs = {}
+
+    def out(name, *shape, dt=torch.float32):
+        bufs[name], view = inside(*shape, dt=dt)
+        return view
+
+    x = torch.randn(N, C, device=DEV)
+    gate = -torch.rand(N, C, device=DEV)
+    p = osdn.make_scan_params(B=1, T=N, C=C, io_dtype="fp32", cu_seqlens=cu)
+    ws = torch.zeros(osdn.osdn_scan_workspace_bytes(p), device=DEV, dtype=torch.uint8)
+    st = torch.randn(3, C, device=DEV)
+    osdn.osdn_scan_fwd(p, x, gate, st, out("h", N, C), out("f", 3, C))
+    osdn.osdn_scan_bwd(p, x, gate, st, x, st, out("dx", N, C), out("dg", N, C), out("di", 3, C), ws)
+    p = osdn.make_conv_params(B=1, T=N, C=C, W=4, io_dtype="fp32", cu_seqlens=cu)
+    w, st = torch.randn(C, 4, device=DEV), torch.randn(3, 3, C, device=DEV)
+    ws = torch.zeros(osdn.osdn_short_conv_workspace_bytes(p), device=DEV, dtype=torch.uint8)
+    osdn.osdn_short_conv_fwd(p, x, w, None, st, out("y", N, C), out("cf", 3, 3, C))
+    osdn.osdn_short_conv_bwd(p, x, w, None, st, x, st, out("cdx", N, C), out("dw", C, 4), None, out("cdi", 3, 3, C), ws)
+    p = osdn.make_qk_norm_params(B=1, T=N, Hq=1, Hk=1, D=C, io_dtype="fp32", rot_dim=16, cu_seqlens=cu)
+    inv = torch.ones(8, device=DEV, dtype=torch.float64)
+    q = x.view(N, 1, C)
+    osdn.osdn_qk_norm_fwd(p, q, q, None, None, inv, None, out("q", N, 1, C), out("k", N, 1, C))
+    osdn.osdn_qk_norm_bwd(p, q, q, None, None, inv, None, q, q, out("dq", N, 1, C), out("dk", N, 1, C), None, None)
+    torch.cuda.synchronize()
+    for name, b in bufs.items():
+        assert bool((b[:guard] == MARK).all()) and bool((b[-guard:] == MARK).all()), name
