@@ -5,6 +5,9 @@ of the layer runs in the CUDA kernels of ``libosdn.so``.  There is no CPU or eag
 fallback: if the library is missing or no CUDA device is present the calls raise.
 
     from paper_2605_13473_b200 import osdn_fwd, osdn_bwd, osdn_precond_update
+
+Operators beside the layer: ``osdn_scan_*`` (gated linear recurrence), ``osdn_short_conv_*`` (short causal
+convolution), ``osdn_qk_norm_*`` (norms of queries and keys with the position rotation).
 """
 from .binding import (  # noqa: F401
     FLAG_RESIDUALS_VALID,
