@@ -296,7 +296,8 @@ int osdn_workspace_region(const osdn_params* p, int need_bwd, const char* name, 
  *   - Token tensors are rows of channels, [tokens, C] row-major: tokens = B T (dense) or T (var-len,
  *     B = 1).  A [T, H, D] tensor is C = H D channels.
  *   - Var-len: sequences may be empty.  A batch may be padded behind its last sequence (cu[nseq] < T):
- *     rows from cu[nseq] on are not read into any result and stay as they were in every output.  A
+ *     rows from cu[nseq] on are not read into any result and stay as they were in every output.  Sequences
+ *     do not touch one another, whatever their values (NaN, infinities).  A
  *     cu_seqlens that breaks its contract otherwise (cu[0] != 0, a decreasing pair, cu[nseq] > T) gives
  *     undefined results, but no access leaves the tensors.
  *   - Inputs are never written.  Outputs may not overlap inputs or one another unless stated.

@@ -319,6 +319,16 @@ template <typename V, bool FLAT, bool SPLIT> struct Stand {
     __device__ __forceinline__ int live(int t) const { return min(max(limit - t, 0), UNIT); }
 };
 
+// The map (g, b) of a stretch on the state in front of it; one in which a sequence begins (g = -inf) takes nothing from it.
+template <int N> __device__ __forceinline__ F<N> apply(const F<N>& g, const F<N>& b, const F<N>& h)
+{
+    const F<N> y = Decay<N>::of(g).step(h, b);
+    F<N> r;
+#pragma unroll
+    for (int k = 0; k < N; ++k) r.x[k] = g.x[k] == -INFINITY ? b.x[k] : y.x[k];
+    return r;
+}
+
 // A split walk's first pass over the CTA's rows: what they do to the state in front of them, as (sum of gates, b), and from
 // the other CTAs' the state in front of this one.  REVERSE: for e = a (y + e), from the end.  Warp 0 has the result.
 template <typename V, bool COMP, bool FLAT, bool REVERSE, typename S>
@@ -408,9 +418,10 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
 #pragma unroll
         for (int k = 0; k < V::WARPS; ++k) {
             const int w = REVERSE ? V::WARPS - 1 - k : k;
-            const F<N> wg = read<N>(&hand.g[w][l]);
-            b = Decay<N>::of(wg).step(b, read<N>(&hand.b[w][l]));
-            g = add(g, wg);
+            const F<N> wg = read<N>(&hand.g[w][l]), sum = add(g, wg);
+            b = apply<N>(wg, read<N>(&hand.b[w][l]), b);
+#pragma unroll
+            for (int k = 0; k < N; ++k) g.x[k] = wg.x[k] == -INFINITY ? wg.x[k] : sum.x[k];
         }
         write<N>(&hand.g[0][l], g);
         write<N>(&hand.b[0][l], b);
@@ -419,7 +430,7 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
     cluster_wait();
     if (at.warp == 0)
         for (int r = REVERSE ? a.span - 1 : 0; r != at.rank; r += REVERSE ? -1 : 1)
-            h = Decay<N>::of(read_remote<N>(&hand.g[0][l], r)).step(h, read_remote<N>(&hand.b[0][l], r));
+            h = apply<N>(read_remote<N>(&hand.g[0][l], r), read_remote<N>(&hand.b[0][l], r), h);
     cluster_arrive();   // nobody leaves, or writes there again, before all have read: waited for at the end
     return h;
 }
@@ -517,14 +528,15 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_fwd_kernel(
         F<N> behind;
         pin<N>(d, b);
         const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
-        if (u > at.first && u + 1 < at.last) {
+        const bool begins = FLAT && marks.first;   // nothing of the state in front reaches the rows behind, not even a NaN
+        if (u > at.first && u + 1 < at.last && !begins) {
             h = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
         } else {
             if (u > at.first) {
                 take_over(at.warp);
                 h = read<N>(&hand.state[at.warp][l]);
             }
-            behind = md.step(h, mb);
+            behind = begins ? mb : md.step(h, mb);
             if (u + 1 < at.last) {
                 write<N>(&hand.state[next][l], behind);
                 hand_on(next);
@@ -668,14 +680,15 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_bwd_kernel(
         F<N> behind;
         pin<N>(d, before);
         const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
-        if (u > at.first && u + 1 < at.last) {
+        const bool ends = FLAT && marks.last;
+        if (u > at.first && u + 1 < at.last && !ends) {
             e = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
         } else {
             if (u + 1 < at.last) {
                 take_over(at.warp);
                 e = read<N>(&hand.state[at.warp][l]);
             }
-            behind = md.step(e, mb);
+            behind = ends ? mb : md.step(e, mb);
             if (u > at.first) {
                 write<N>(&hand.state[next][l], behind);
                 hand_on(next);

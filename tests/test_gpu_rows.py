@@ -634,3 +634,34 @@ def test_broken_boundaries_stay_inside_the_tensors(broken):
     torch.cuda.synchronize()
     for name, b in bufs.items():
         assert bool((b[:guard] == MARK).all()) and bool((b[-guard:] == MARK).all()), name
+
+
+@pytest.mark.parametrize("lens,bad", [([3, 2, 4, 1, 70], 1), ([100, 37, 300, 0, 5], 2), ([20000, 5, 12000, 3000], 1), ([9000, 16000, 7000], 1)])
+def test_a_sequence_of_nan_and_infinities_stays_alone(lens, bad):
+    """Neighbours in a packed batch get what they get beside finite values, forward and backward, across CTAs and clusters."""
+    C, N = 64, sum(lens)
+    lo = sum(lens[:bad])
+    hi = lo + lens[bad]
+    g = _gen(N)
+    x, gate = _scan_inputs(N, C, "fp32", N)
+    dout, init, dfin = torch.randn(N, C, generator=g), torch.randn(len(lens), C, generator=g), torch.randn(len(lens), C, generator=g)
+    w = torch.randn(C, 4, generator=g)
+    cinit, cdfin = (torch.randn(len(lens), 3, C, generator=g) for _ in range(2))
+    keep = torch.ones(N, dtype=torch.bool)
+    keep[lo:hi] = False
+    others = [s for s in range(len(lens)) if s != bad]
+    for poison in ("values", "gates"):
+        px, pg, pd = x.clone(), gate.clone(), dout.clone()
+        (px if poison == "values" else pg)[lo:hi] = float("nan")
+        px[lo:hi, ::2] = float("inf")
+        pd[lo:hi, 1::2] = float("-inf")
+        a = _run_scan(x, gate, lens, False, C, "fp32", False, init, dout, dfin)
+        b = _run_scan(px, pg, lens, False, C, "fp32", False, init, pd, dfin)
+        for k, (u, v) in enumerate(zip(a, b)):
+            m = keep if k in (0, 2, 3) else others
+            assert torch.equal(u[m], v[m]), (poison, k)
+        a = _run_conv(x, w, None, lens, False, "fp32", True, cinit, dout, cdfin)
+        b = _run_conv(px, w, None, lens, False, "fp32", True, cinit, pd, cdfin)
+        for k in (0, 1, 2, 5):
+            m = keep if k in (0, 2) else others
+            assert torch.equal(a[k][m], b[k][m]), (poison, k)
