@@ -463,8 +463,6 @@ ConvArgs make_args(const osdn_conv_params& p)
     return a;
 }
 
-template <typename T> constexpr int kWide = sizeof(T) == 2 ? 8 : 4;   // channels of a 16-byte access
-
 // Channels to a lane: rows that are whole 16-byte pieces are staged.
 int lane_channels(const osdn_conv_params& p)
 {
@@ -581,12 +579,14 @@ int conv_step(const osdn_conv_params& p, const void* x, const float* w, const fl
         auto go = [&](auto vec) {
             constexpr int N = decltype(vec)::value;
             const long long n = p.C / N;
-            const int each = (int)std::max(1ll, std::min(4ll, p.B * n / (148 * 256)));   // the taps are as many bytes as a row
+            // the taps are as many bytes as a row of two sequences (512 sequences, 2048 channels: one to a thread 6.3 us, two 5.3,
+            // four 7.0; with eight channels to a lane 7.1 and more)
+            const int each = (int)std::max(1ll, std::min(2ll, p.B * n / (148 * 256)));
             return launch_after(conv_step_kernel<T, N, W, SILU>, dim3(div_up(div_up(p.B, each) * n, 128)), dim3(128), 0, st,
                                 static_cast<const T*>(x), w, bias, static_cast<T*>(state), static_cast<T*>(out), p.B, p.T, p.C, each)
                        ? 1 : -1;
         };
-        return p.C % kWide<T> == 0 ? go(std::integral_constant<int, kWide<T>>{}) : go(std::integral_constant<int, 1>{});
+        return p.C % 4 == 0 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 1>{});
     });
     stage_end(st);
     return launched;
