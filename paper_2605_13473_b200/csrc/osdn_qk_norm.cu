@@ -278,7 +278,7 @@ template <typename T, int TENSORS, int DEPTH_> struct Ahead {
         for (slot = 0; slot < DEPTH; ++slot) ask(a);
         slot = 0;
     }
-    __device__ __forceinline__ void next(const NormArgs& a, Channels<T, 8> (&raw)[TENSORS])
+    __device__ __forceinline__ void read(Channels<T, 8> (&raw)[TENSORS]) const
     {
         copies_wait<DEPTH - 1>();
 #pragma unroll
@@ -288,6 +288,10 @@ template <typename T, int TENSORS, int DEPTH_> struct Ahead {
                 const uint4 v = *reinterpret_cast<const uint4*>(at(slot, t) + p * 256 * 16);
                 raw[t].w[4 * p] = v.x; raw[t].w[4 * p + 1] = v.y; raw[t].w[4 * p + 2] = v.z; raw[t].w[4 * p + 3] = v.w;
             }
+    }
+    // Behind the store of what was made of the last read: nothing of it is still on its way out of the place.
+    __device__ __forceinline__ void refill(const NormArgs& a)
+    {
         ask(a);
         slot = slot + 1 < DEPTH ? slot + 1 : 0;
     }
@@ -351,9 +355,10 @@ __global__ void __launch_bounds__(256, BWD_CTAS) qk_norm_bwd_kernel(NormArgs a)
             w.load(part ? a.kw : a.qw, f0, rows.in);
             for (int h = 0; h < H; ++h, to += a.D) {
                 Channels<T, 8> raw[2];
-                rows.next(a, raw);
+                rows.read(raw);
                 const Channels<T, 8> y = norm_head_bwd<T, LH, ROT, WEIGHTS>(a, r, w, dw[part], f0, raw[0], raw[1]);
                 if (live && rows.in) y.store(to);
+                rows.refill(a);
             }
         }
     }
