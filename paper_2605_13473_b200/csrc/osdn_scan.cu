@@ -284,7 +284,8 @@ __device__ __forceinline__ int previous(const ScanArgs& a, int q)
 
 template <typename V> struct Hand {
     float state[V::WARPS][V::CB];                    // in front of the unit that warp w takes next
-    float g[V::WARPS][V::CB], b[V::WARPS][V::CB];    // a split walk: the maps of the warps' stretches, then [0] the CTA's
+    float g[V::WARPS][V::CB], b[V::WARPS][V::CB];    // a split walk: the maps of the warps' stretches
+    float all_g[V::CB], all_b[V::CB];                //   and the CTA's
 };
 
 // A state of an empty sequence (or its gradient) passes through; `place` of `places` warps of the walk.
@@ -329,17 +330,16 @@ template <int N> __device__ __forceinline__ F<N> apply(const F<N>& g, const F<N>
     return r;
 }
 
-// A split walk's first pass over the CTA's rows: what they do to the state in front of them, as (sum of gates, b), and from
-// the other CTAs' the state in front of this one.  REVERSE: for e = a (y + e), from the end.  Warp 0 has the result.
+// A split walk's first pass over the rows of this warp, units lo .. hi-1: what they do to the state in front of them, as (sum of
+// gates, b), and from the other CTAs' and warps' the state in front of this warp's.  REVERSE: for e = a (y + e), from the end.
 template <typename V, bool COMP, bool FLAT, bool REVERSE, typename S>
 __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& at, Hand<V>& hand, F<V::VEC> h, const float* gate,
-                                                    const typename V::T* x, char* part, int bytes)
+                                                    const typename V::T* x, char* part, int bytes, int lo, int hi)
 {
     using FetchG = Fetch<float, V>;
     using FetchX = Fetch<typename V::T, V>;
     constexpr int N = V::VEC;
-    const int l = (threadIdx.x & 31) * N, per = (at.last - at.first + V::WARPS - 1) / V::WARPS;
-    const int lo = min(at.first + at.warp * per, at.last), hi = min(lo + per, at.last);
+    const int l = (threadIdx.x & 31) * N;
     auto unit = [&](int i) { return REVERSE ? hi - 1 - i : lo + i; };
     auto ask = [&](int i, int place) {
         if (i < hi - lo) {
@@ -423,14 +423,15 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
 #pragma unroll
             for (int k = 0; k < N; ++k) g.x[k] = wg.x[k] == -INFINITY ? wg.x[k] : sum.x[k];
         }
-        write<N>(&hand.g[0][l], g);
-        write<N>(&hand.b[0][l], b);
+        write<N>(&hand.all_g[l], g);
+        write<N>(&hand.all_b[l], b);
     }
     cluster_arrive();
     cluster_wait();
-    if (at.warp == 0)
-        for (int r = REVERSE ? a.span - 1 : 0; r != at.rank; r += REVERSE ? -1 : 1)
-            h = apply<N>(read_remote<N>(&hand.g[0][l], r), read_remote<N>(&hand.b[0][l], r), h);
+    for (int r = REVERSE ? a.span - 1 : 0; r != at.rank; r += REVERSE ? -1 : 1)
+        h = apply<N>(read_remote<N>(&hand.all_g[l], r), read_remote<N>(&hand.all_b[l], r), h);
+    for (int w = REVERSE ? V::WARPS - 1 : 0; w != at.warp; w += REVERSE ? -1 : 1)
+        h = apply<N>(read<N>(&hand.g[w][l]), read<N>(&hand.b[w][l]), h);
     cluster_arrive();   // nobody leaves, or writes there again, before all have read: waited for at the end
     return h;
 }
@@ -465,9 +466,12 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_fwd_kernel(
     if (FLAT && a.cu && a.fin && at.inside) pass_empty<N>(a, a.init, a.fin, at.rank * V::WARPS + at.warp, a.span * V::WARPS, c);
     F<N> h = all<N>(0.f);
     if (!FLAT && at.inside) h = read_or_zero<N>(a.init, (size_t)at.s * a.C + c);
-    if (SPLIT) h = state_in_front<V, COMP, FLAT, false>(a, at, hand, h, gate, x, part, PART);
+    // this warp's units: in turn with the others', or a stretch of its own whose state in front is known
+    const int per = (at.last - at.first + V::WARPS - 1) / V::WARPS, pitch = SPLIT ? 1 : V::WARPS;
+    const int lo = SPLIT ? min(at.first + at.warp * per, at.last) : at.first + at.warp, hi = SPLIT ? min(lo + per, at.last) : at.last;
+    if (SPLIT) h = state_in_front<V, COMP, FLAT, false>(a, at, hand, h, gate, x, part, PART, lo, hi);
     auto ask = [&](int u, int place) {
-        if (u < at.last) {
+        if (u < hi) {
             const int t = u * UNIT, live = at.live(t);
             const size_t row = live ? (size_t)t * a.C : 0;
             FetchG::ask(part + place * PART, gate + row, a.C, live, a.C - at.c0);
@@ -476,10 +480,10 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_fwd_kernel(
         copies_end();
     };
     Marks marks;
-    int u = at.first + at.warp, place = 0;
+    int u = lo, place = 0;
     if (V::STAGED)
-        for (int i = 0; i < V::DEPTH; ++i) ask(u + i * V::WARPS, i);
-    for (; u < at.last; u += V::WARPS) {
+        for (int i = 0; i < V::DEPTH; ++i) ask(u + i * pitch, i);
+    for (; u < hi; u += pitch) {
         const int t = u * UNIT, live = at.live(t);
         const size_t row = (size_t)t * a.C;
         if (FLAT) marks.find(a, t, UNIT, at.limit);
@@ -493,7 +497,7 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_fwd_kernel(
         fg.take(part + place * PART, gate + row, a.C, live, c - at.c0, at.inside);
         fx.take(part + place * PART + FetchG::BYTES, x + row, a.C, live, c - at.c0, at.inside);
         __syncwarp();
-        if (V::STAGED) ask(u + V::DEPTH * V::WARPS, place);
+        if (V::STAGED) ask(u + V::DEPTH * pitch, place);
         place = place + 1 < V::DEPTH ? place + 1 : 0;
         Decay<N> d[UNIT];
         F<N> b[UNIT];
@@ -510,9 +514,10 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_fwd_kernel(
 #pragma unroll
             for (int i = j; i < j + SIDE; ++i) b[i] = COMP ? mul(d[i].complement(), fx.r[i].get()) : fx.r[i].get();
 #pragma unroll
-            for (int i = j; i < j + SIDE; ++i) mb = d[i].step(mb, b[i]);
+            for (int i = j; i < j + SIDE; ++i)
+                if (!SPLIT) mb = d[i].step(mb, b[i]);
         }
-        if (FLAT && marks.first) {
+        if (!SPLIT && FLAT && marks.first) {
             int q = marks.s;
 #pragma unroll
             for (int i = 0; i < UNIT; ++i) {
@@ -524,25 +529,27 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_fwd_kernel(
             }
             mg = all<N>(-INFINITY);
         }
-        const Decay<N> md = Decay<N>::of(mg);
-        F<N> behind;
         pin<N>(d, b);
-        const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
-        const bool begins = FLAT && marks.first;   // nothing of the state in front reaches the rows behind, not even a NaN
-        if (u > at.first && u + 1 < at.last && !begins) {
-            h = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
-        } else {
-            if (u > at.first) {
-                take_over(at.warp);
-                h = read<N>(&hand.state[at.warp][l]);
+        if constexpr (!SPLIT) {
+            const Decay<N> md = Decay<N>::of(mg);
+            F<N> behind;
+            const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
+            const bool begins = FLAT && marks.first;   // nothing of the state in front reaches the rows behind, not even a NaN
+            if (u > at.first && u + 1 < at.last && !begins) {
+                h = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
+            } else {
+                if (u > at.first) {
+                    take_over(at.warp);
+                    h = read<N>(&hand.state[at.warp][l]);
+                }
+                behind = begins ? mb : md.step(h, mb);
+                if (u + 1 < at.last) {
+                    write<N>(&hand.state[next][l], behind);
+                    hand_on(next);
+                }
             }
-            behind = begins ? mb : md.step(h, mb);
-            if (u + 1 < at.last) {
-                write<N>(&hand.state[next][l], behind);
-                hand_on(next);
-            }
+            if (!FLAT && a.fin && u + 1 == a.units && at.inside) write<N>(a.fin + (size_t)at.s * a.C + c, behind);
         }
-        if (!FLAT && a.fin && u + 1 == a.units && at.inside) write<N>(a.fin + (size_t)at.s * a.C + c, behind);
         if (plain) {
             if (saved) write<N>(saved + (size_t)u * a.C, h);
 #pragma unroll
@@ -565,6 +572,7 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_fwd_kernel(
                 if (FLAT && a.fin && (marks.last >> i & 1)) write<N>(a.fin + (size_t)q * a.C + c, h);
             }
         }
+        if (SPLIT && !FLAT && a.fin && u + 1 == a.units && at.inside) write<N>(a.fin + (size_t)at.s * a.C + c, h);
     }
     if (SPLIT) cluster_wait();
 }
@@ -594,9 +602,12 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_bwd_kernel(
     if (FLAT && a.cu && a.dinit && at.inside) pass_empty<N>(a, a.dfin, a.dinit, at.rank * V::WARPS + at.warp, a.span * V::WARPS, c);
     F<N> e = all<N>(0.f);
     if (!FLAT && at.inside) e = read_or_zero<N>(a.dfin, (size_t)at.s * a.C + c);
-    if (SPLIT) e = state_in_front<V, COMP, FLAT, true>(a, at, hand, e, gate, dout, part, PART);
+    const int per = (at.last - at.first + V::WARPS - 1) / V::WARPS, pitch = SPLIT ? 1 : V::WARPS;
+    const int lo = SPLIT ? min(at.first + at.warp * per, at.last) : at.first;
+    const int hi = SPLIT ? min(lo + per, at.last) : at.last - at.warp;
+    if (SPLIT) e = state_in_front<V, COMP, FLAT, true>(a, at, hand, e, gate, dout, part, PART, lo, hi);
     auto ask = [&](int u, int place) {
-        if (u >= at.first) {
+        if (u >= lo) {
             const int t = u * UNIT, live = at.live(t);
             const size_t row = live ? (size_t)t * a.C : 0;
             char* const to = part + place * PART;
@@ -607,10 +618,10 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_bwd_kernel(
         copies_end();
     };
     Marks marks;
-    int u = at.last - 1 - at.warp, place = 0;
+    int u = hi - 1, place = 0;
     if (V::STAGED)
-        for (int i = 0; i < V::DEPTH; ++i) ask(u - i * V::WARPS, i);
-    for (; u >= at.first; u -= V::WARPS) {
+        for (int i = 0; i < V::DEPTH; ++i) ask(u - i * pitch, i);
+    for (; u >= lo; u -= pitch) {
         const int t = u * UNIT, live = at.live(t);
         const size_t row = (size_t)t * a.C;
         if (FLAT) marks.find(a, t, UNIT, at.limit);
@@ -628,7 +639,7 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_bwd_kernel(
         fx.take(from + FetchG::BYTES, x + row, a.C, live, c - at.c0, at.inside);
         fy.take(from + FetchG::BYTES + FetchX::BYTES, dout + row, a.C, live, c - at.c0, at.inside);
         __syncwarp();
-        if (V::STAGED) ask(u - V::DEPTH * V::WARPS, place);
+        if (V::STAGED) ask(u - V::DEPTH * pitch, place);
         place = place + 1 < V::DEPTH ? place + 1 : 0;
         Decay<N> d[UNIT];
         F<N> before[UNIT];
@@ -652,7 +663,8 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_bwd_kernel(
                 h = d[i].step(h, COMP ? mul(d[i].complement(), y) : y);
             }
 #pragma unroll
-            for (int i = UNIT - 1; i >= 0; --i) mb = d[i].times(add(fy.r[i].get(), mb));
+            for (int i = UNIT - 1; i >= 0; --i)
+                if (!SPLIT) mb = d[i].times(add(fy.r[i].get(), mb));
         } else {
             int q = marks.s;
 #pragma unroll
@@ -676,25 +688,27 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_bwd_kernel(
                 if (i && (marks.first >> i & 1)) q = previous(a, q);
             }
         }
-        const Decay<N> md = Decay<N>::of(mg);
-        F<N> behind;
         pin<N>(d, before);
-        const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
-        const bool ends = FLAT && marks.last;
-        if (u > at.first && u + 1 < at.last && !ends) {
-            e = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
-        } else {
-            if (u + 1 < at.last) {
-                take_over(at.warp);
-                e = read<N>(&hand.state[at.warp][l]);
+        if constexpr (!SPLIT) {
+            const Decay<N> md = Decay<N>::of(mg);
+            F<N> behind;
+            const int next = at.warp + 1 < V::WARPS ? at.warp + 1 : 0;
+            const bool ends = FLAT && marks.last;
+            if (u > at.first && u + 1 < at.last && !ends) {
+                e = relay<N>(at.warp, next, &hand.state[at.warp][l], &hand.state[next][l], md, mb, behind);
+            } else {
+                if (u + 1 < at.last) {
+                    take_over(at.warp);
+                    e = read<N>(&hand.state[at.warp][l]);
+                }
+                behind = ends ? mb : md.step(e, mb);
+                if (u > at.first) {
+                    write<N>(&hand.state[next][l], behind);
+                    hand_on(next);
+                }
             }
-            behind = ends ? mb : md.step(e, mb);
-            if (u > at.first) {
-                write<N>(&hand.state[next][l], behind);
-                hand_on(next);
-            }
+            if (!FLAT && a.dinit && u == 0 && at.inside) write<N>(a.dinit + (size_t)at.s * a.C + c, behind);
         }
-        if (!FLAT && a.dinit && u == 0 && at.inside) write<N>(a.dinit + (size_t)at.s * a.C + c, behind);
         if (plain) {
 #pragma unroll
             for (int i = UNIT - 1; i >= 0; --i) {
@@ -719,6 +733,7 @@ __global__ void __launch_bounds__(32 * V::WARPS, 16 / V::WARPS) scan_bwd_kernel(
                 }
             }
         }
+        if (SPLIT && !FLAT && a.dinit && u == 0 && at.inside) write<N>(a.dinit + (size_t)at.s * a.C + c, e);
     }
     if (SPLIT) cluster_wait();
 }
