@@ -443,7 +443,8 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
 // all warps instead, tile by tile, the warps waited more than they worked (8 x 2048 tokens, 1024 channels, bf16: 38 to 51 us;
 // so 27.3, 4.9 TB/s of what has to be read and written, and the backward 41.5, 5.7 TB/s).  29 instructions an element, of which
 // the factor takes nine; bound by their issue and latency in bf16, by memory in fp32 (5.9 TB/s).
-// Few walks are split among the CTAs of a cluster, which read their rows once more for the state in front of them.
+// Few walks are split among the warps of a cluster's CTAs, a stretch of rows to each, read once more for the state in front of
+// it: then nothing is waited for but rows (131072 tokens, 1024 channels: 415 us, 39 % of the bytes' rate; by the relay 490).
 // Rows that are all there and begin and end no sequence take the code without tests.
 // out == nullptr: only the states are kept.
 template <typename V, bool COMP, bool FLAT, bool SPLIT>
@@ -793,11 +794,16 @@ int span_of(long long walks, int units, int warps)
 // Warps of a CTA.  Sixteen where an SM has one CTA with enough units for them, eight where it has two or the walk is short
 // (forward, 1024 channels, sixteen and eight: 8 x 2048 tokens 28.7 and 29.4 us, backward 40.9 and 52.1; 32 x 2048 106 and
 // 97; 64 x 100 23.5 and 15.4; one of 2048 22.0 and 15.7).
-int warps_of(const ScanArgs& a, bool flat, int channels)
+struct Shape {
+    int warps;
+    bool split;
+};
+Shape shape_of(const ScanArgs& a, bool flat)
 {
-    const long long walks = (long long)(flat ? 1 : a.S) * div_up(a.C, channels);
+    const long long walks = (long long)(flat ? 1 : a.S) * div_up(a.C, 64);
     const int span = span_of(walks, a.units, 16);
-    return walks < 240 && a.units / span >= (span > 1 ? 256 : 64) ? 16 : 8;
+    const int warps = walks < 240 && a.units / span >= (span > 1 ? 256 : 64) ? 16 : 8;
+    return {warps, span_of(walks, a.units, warps) > 1};
 }
 
 // Kernel(SPLIT) for the walks of a batch.
@@ -839,7 +845,9 @@ template <typename T, bool COMP> bool launch_forward(const ScanArgs& a, bool fla
         return launch_walks<V>(kernel, a, flat, Fetch<float, V>::BYTES + Fetch<T, V>::BYTES, st);
     };
     if (!is_wide<T>(a.C)) return go(Cover<T, 1, 8, 1>{});
-    return warps_of(a, flat, 64) == 16 ? go(Cover<T, 2, 16, 1>{}) : go(Cover<T, 2, 8, 2>{});
+    const Shape f = shape_of(a, flat);   // a split walk's warps wait for nothing but their rows: more of them on their way
+    if (f.warps == 16) return f.split ? go(Cover<T, 2, 16, 3>{}) : go(Cover<T, 2, 16, 1>{});
+    return f.split ? go(Cover<T, 2, 8, 3>{}) : go(Cover<T, 2, 8, 2>{});
 }
 
 template <typename T, bool COMP> int run_backward(const ScanArgs& a, bool flat, bool saved, cudaStream_t st)
@@ -857,9 +865,12 @@ template <typename T, bool COMP> int run_backward(const ScanArgs& a, bool flat, 
         };
         return launch_walks<V>(kernel, a, flat, Fetch<float, V>::BYTES + 2 * Fetch<T, V>::BYTES, st);
     };
-    const bool ok = !is_wide<T>(a.C)               ? go(Cover<T, 1, 8, 1>{})
-                    : warps_of(a, flat, 64) == 16 ? go(Cover<T, 2, 16, 2>{})
-                                                  : go(Cover<T, 2, 8, 2>{});
+    constexpr int MORE = sizeof(T) == 2 ? 3 : 2;
+    const Shape f = shape_of(a, flat);
+    const bool ok = !is_wide<T>(a.C)  ? go(Cover<T, 1, 8, 1>{})
+                    : f.warps == 16  ? (f.split ? go(Cover<T, 2, 16, MORE>{}) : go(Cover<T, 2, 16, 2>{}))
+                    : f.split        ? go(Cover<T, 2, 8, MORE>{})
+                                     : go(Cover<T, 2, 8, 2>{});
     return ok ? n : -1;
 }
 
