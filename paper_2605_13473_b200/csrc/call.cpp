@@ -37,6 +37,7 @@ struct Expect {
     int64_t row = 0;      // elements from one token to the next where that is not the packed width
     int64_t width = 0;    // elements of a token's row (row != 0)
     int64_t head = 0;     //   and of its heads
+    int64_t tokens = 0;
 };
 
 struct Shape {   // tokens and sequences of a batch
@@ -87,7 +88,7 @@ void expect(long which, const void* params, Expect* e)
     } else {
         const auto& p = *static_cast<const osdn_qk_norm_params*>(params);
         const int64_t tok = shape_of(p).tokens, wq = (int64_t)p.Hq * p.D, wk = (int64_t)p.Hk * p.D;
-        const Expect in[] = {{"q", IO, tok * wq, p.q_row, wq, p.D}, {"k", IO, tok * wk, p.k_row, wk, p.D},
+        const Expect in[] = {{"q", IO, tok * wq, p.q_row, wq, p.D, tok}, {"k", IO, tok * wk, p.k_row, wk, p.D, tok},
                              {"q_weight", F32, p.D}, {"k_weight", F32, p.D}, {"inv_freq", F64, p.rot_dim / 2},
                              {"positions", I32, tok}};
         e = std::copy(std::begin(in), std::end(in), e);
@@ -95,39 +96,34 @@ void expect(long which, const void* params, Expect* e)
             const Expect x[] = {{"q_out", IO, tok * wq}, {"k_out", IO, tok * wk}};
             std::copy(std::begin(x), std::end(x), e);
         } else {
-            const Expect x[] = {{"dq_out", IO, tok * wq}, {"dk_out", IO, tok * wk}, {"dq", IO, tok * wq, p.dq_row, wq, p.D},
-                                {"dk", IO, tok * wk, p.dk_row, wk, p.D}, {"dq_weight", F32, p.D}, {"dk_weight", F32, p.D},
+            const Expect x[] = {{"dq_out", IO, tok * wq}, {"dk_out", IO, tok * wk}, {"dq", IO, tok * wq, p.dq_row, wq, p.D, tok},
+                                {"dk", IO, tok * wk, p.dk_row, wk, p.D, tok}, {"dq_weight", F32, p.D}, {"dk_weight", F32, p.D},
                                 {"workspace", BYTES, -1}};
             std::copy(std::begin(x), std::end(x), e);
         }
     }
 }
 
-// Whether a [tokens, heads, D] (or [tokens, width]) view steps through memory as the params say.
+// Whether a tensor steps through memory as the params say: contiguous, or a [tokens, heads, D] or [tokens, width] view of wider
+// rows.  The kernels take `tokens` steps of `row`, so that a view of as many elements in fewer or other rows ends too early.
 bool rows_match(const at::Tensor& t, const Expect& e)
 {
     if (e.row == 0 || e.row == e.width) return t.is_contiguous();
-    if (t.dim() == 2) return t.size(1) == e.width && t.stride(1) == 1 && (t.size(0) == 1 || t.stride(0) == e.row);
-    return t.dim() == 3 && t.size(2) == e.head && t.stride(2) == 1 && (t.size(1) == 1 || t.stride(1) == e.head) &&
-           (t.size(0) == 1 || t.stride(0) == e.row);
+    if (t.dim() < 2 || t.size(0) != e.tokens || (e.tokens > 1 && t.stride(0) != e.row)) return false;
+    if (t.dim() == 2) return t.size(1) == e.width && t.stride(1) == 1;
+    return t.dim() == 3 && t.size(2) == e.head && t.size(1) * e.head == e.width && t.stride(2) == 1 &&
+           (t.size(1) == 1 || t.stride(1) == e.head);
 }
 
-bool checked_pointer(PyObject* o, const Expect& e, bool bf16, int device, void** out, size_t* bytes)
+// Type, size and layout; the device is asked for once all of them are what they have to be.
+bool checked_layout(PyObject* o, const Expect& e, bool bf16)
 {
-    if (o == Py_None) {
-        *out = nullptr;
-        if (e.type == BYTES) *bytes = 0;
-        return true;
-    }
+    if (o == Py_None) return true;
     if (!THPVariable_Check(o)) {
         PyErr_Format(PyExc_TypeError, "%s: the OSDN library takes torch tensors (or None)", e.name);
         return false;
     }
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.is_cuda() || t.get_device() != device) {
-        PyErr_Format(PyExc_ValueError, "%s: not on the current CUDA device", e.name);
-        return false;
-    }
     const at::ScalarType want = e.type == IO ? (bf16 ? at::kBFloat16 : at::kFloat)
                                 : e.type == F32 ? at::kFloat : e.type == F64 ? at::kDouble : at::kInt;
     if (e.type != BYTES && t.scalar_type() != want) {
@@ -140,6 +136,21 @@ bool checked_pointer(PyObject* o, const Expect& e, bool bf16, int device, void**
     }
     if (!rows_match(t, e)) {
         PyErr_Format(PyExc_ValueError, e.row ? "%s: rows are not laid out as the params say" : "%s: must be contiguous", e.name);
+        return false;
+    }
+    return true;
+}
+
+bool checked_pointer(PyObject* o, const Expect& e, int device, void** out, size_t* bytes)
+{
+    if (o == Py_None) {
+        *out = nullptr;
+        if (e.type == BYTES) *bytes = 0;
+        return true;
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.get_device() != device) {
+        PyErr_Format(PyExc_ValueError, "%s: not on the current CUDA device", e.name);
         return false;
     }
     *out = t.data_ptr();
@@ -275,14 +286,12 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n)
     try {
         if (ok && kind != LAYER) {
             Expect e[13];
-            int device = -1;
             const bool valid = valid_rows(which, view.buf);   // if not, the library says why
-            if (valid) {
-                expect(which, view.buf, e);
-                device = c10::cuda::current_device();
-            }
             const bool bf16 = is_bf16(which, view.buf);
-            for (Py_ssize_t i = 0; ok && valid && i < n - 2; ++i) ok = checked_pointer(args[2 + i], e[i], bf16, device, &x[i], &bytes);
+            if (valid) expect(which, view.buf, e);
+            for (Py_ssize_t i = 0; ok && valid && i < n - 2; ++i) ok = checked_layout(args[2 + i], e[i], bf16);
+            const int device = ok && valid ? c10::cuda::current_device() : -1;
+            for (Py_ssize_t i = 0; ok && valid && i < n - 2; ++i) ok = checked_pointer(args[2 + i], e[i], device, &x[i], &bytes);
             if (!valid) std::fill(std::begin(x), std::end(x), nullptr);
             if (ok) {
                 void* st = valid ? c10::cuda::getCurrentCUDAStream().stream() : nullptr;

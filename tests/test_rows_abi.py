@@ -209,3 +209,41 @@ def test_marshalled_calls_check_their_tensors():
         osdn.osdn_qk_norm_fwd(norm_params(q_row=512, k_row=640), q, k, None, None, None, None, y, yk)
     with pytest.raises(ValueError, match="q: rows"):
         osdn.osdn_qk_norm_fwd(norm_params(q_row=512, k_row=512), q.transpose(0, 1), k, None, None, None, None, y, yk)
+
+
+@pytest.mark.parametrize("name", ["q", "k", "dq", "dk"])
+@pytest.mark.parametrize("io", ["bf16", "fp32"])
+def test_views_of_as_many_elements_in_other_rows_are_refused(lib, name, io):
+    """A view that steps by the params' row but has fewer (or other) rows ends before the kernels' last token.  Told from the
+    shapes alone, before any device is asked for."""
+    T, H, D, row = 8, 2, 16, 160
+    dt = {"bf16": torch.bfloat16, "fp32": torch.float32}[io]
+    p = osdn.make_qk_norm_params(B=1, T=T, Hq=H, Hk=H, D=D, io_dtype=io, **{name + "_row": row})
+    packed = {n: torch.zeros(T, H, D, dtype=dt) for n in ("q", "k", "q_out", "k_out", "dq", "dk")}
+    wide = torch.zeros(T, row, dtype=dt)
+    fits = [wide[:, :H * D].view(T, H, D), wide[:, 32:32 + H * D]]
+    short = [wide[:T // 2, :2 * H * D].view(T // 2, 2 * H, D), torch.zeros(1, T * H, D, dtype=dt), wide[:T // 4, :4 * H * D].view(2, 8, D),
+             wide[:T // 2, :2 * H * D], torch.zeros(1, T * H * D, dtype=dt), torch.zeros(T * H * D, dtype=dt)]
+    other = [wide[:, :H * D].view(T, H, D).flip(0).transpose(1, 2), wide.view(2, T // 2, row)[:, :, :H * D],
+             torch.zeros(T, H * row, dtype=dt).view(T, H, row)[:, :, :D]]
+
+    def call(view):
+        t = packed | {name: view}
+        if name in "qk":
+            osdn.osdn_qk_norm_fwd(p, t["q"], t["k"], None, None, None, None, t["q_out"], t["k_out"])
+        else:
+            osdn.osdn_qk_norm_bwd(p, t["q"], t["k"], None, None, None, None, t["q_out"], t["k_out"], t["dq"], t["dk"], None, None)
+
+    for view in short + other:
+        assert view.numel() == T * H * D
+        with pytest.raises(ValueError, match=name + ": rows are not laid out as the params say"):
+            call(view)
+    for view in fits:                # only where the tensors are is left to complain about
+        with pytest.raises((ValueError, RuntimeError)) as e:
+            call(view)
+        assert "rows" not in str(e.value) and "elements" not in str(e.value)
+    one = osdn.make_qk_norm_params(B=1, T=1, Hq=H, Hk=H, D=D, io_dtype=io, **{name + "_row": row})
+    p, packed = one, {n: v[:1] for n, v in packed.items()}
+    with pytest.raises((ValueError, RuntimeError)) as e:      # one token: no step to compare
+        call(torch.zeros(1, H, D, dtype=dt))
+    assert "rows" not in str(e.value)
