@@ -338,7 +338,7 @@ def osdn_step_host(p: OsdnParams, q, k, v, beta, gate, dout, out, dq, dk, dv, db
 # Operators beside the layer: the gated linear recurrence, the short causal convolution, the norms of queries and
 # keys.  Shapes and meanings: include/osdn.h.  Tensors have to be on the current CUDA device, of the dtype and size that
 # the params say, and contiguous (q, k, dq, dk: or [tokens, heads, D] or [tokens, heads D] views of wider rows, as the params
-# say); a ValueError tells which one is not.
+# say); a ValueError tells which one is not.  So has the cu_seqlens that the params were made with, whenever they are used.
 # ---------------------------------------------------------------------------------------------
 def _batch(p, B, T, io_dtype, cu_seqlens, flags):
     p.B, p.T, p.io_dtype, p.flags = B, T, {"fp32": 0, "bf16": 1}[io_dtype], flags

@@ -254,6 +254,31 @@ bool is_bf16(long which, const void* params)
     }
 }
 
+// Packed batches: the tensor that the params' cu_seqlens points into is on the device as well.  (Params whose pointer the caller has
+// set by hand have none, and nothing is known of it.)
+bool checked_boundaries(long which, const void* params, PyObject* object, int device)
+{
+    const Params kind = params_of(which);
+    const int32_t nseq = kind == SCAN   ? static_cast<const osdn_scan_params*>(params)->nseq
+                         : kind == CONV ? static_cast<const osdn_conv_params*>(params)->nseq
+                                        : static_cast<const osdn_qk_norm_params*>(params)->nseq;
+    if (nseq == 0) return true;
+    PyObject* const o = PyObject_GetAttrString(object, "_cu_seqlens");
+    if (!o) {
+        if (!PyErr_ExceptionMatches(PyExc_AttributeError)) return false;
+        PyErr_Clear();
+        return true;
+    }
+    bool ok = true;
+    if (THPVariable_Check(o)) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        ok = t.is_cuda() && t.get_device() == device;
+    }
+    Py_DECREF(o);
+    if (!ok) PyErr_SetString(PyExc_ValueError, "cu_seqlens: not on the current CUDA device");
+    return ok;
+}
+
 // call(which, params, *tensors) -> status code of the library
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -292,6 +317,7 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n)
             for (Py_ssize_t i = 0; ok && valid && i < n - 2; ++i) ok = checked_layout(args[2 + i], e[i], bf16);
             const int device = ok && valid ? c10::cuda::current_device() : -1;
             for (Py_ssize_t i = 0; ok && valid && i < n - 2; ++i) ok = checked_pointer(args[2 + i], e[i], device, &x[i], &bytes);
+            if (ok && valid) ok = checked_boundaries(which, view.buf, args[1], device);
             if (!valid) std::fill(std::begin(x), std::end(x), nullptr);
             if (ok) {
                 void* st = valid ? c10::cuda::getCurrentCUDAStream().stream() : nullptr;

@@ -247,3 +247,28 @@ def test_views_of_as_many_elements_in_other_rows_are_refused(lib, name, io):
     with pytest.raises((ValueError, RuntimeError)) as e:      # one token: no step to compare
         call(torch.zeros(1, H, D, dtype=dt))
     assert "rows" not in str(e.value)
+
+
+@pytest.mark.gpu
+def test_boundaries_elsewhere_are_refused():
+    """cu_seqlens of another device would be read by the kernels of this one.  (Here: params whose tensor is host memory; what
+    they point at is never followed.)"""
+    d = "cuda:0"
+    cu = torch.tensor([0, 3, 8], dtype=torch.int32, device=d)
+    x, g, w, q = torch.randn(8, 16, device=d), -torch.rand(8, 16, device=d), torch.randn(16, 4, device=d), torch.randn(8, 2, 8, device=d)
+    y, yq, yk = torch.empty_like(x), torch.empty_like(q), torch.empty_like(q)
+    calls = [(osdn.make_scan_params(B=1, T=8, C=16, io_dtype="fp32", cu_seqlens=cu), lambda p: osdn.osdn_scan_fwd(p, x, g, None, y, None)),
+             (osdn.make_conv_params(B=1, T=8, C=16, W=4, io_dtype="fp32", cu_seqlens=cu),
+              lambda p: osdn.osdn_short_conv_fwd(p, x, w, None, None, y, None)),
+             (osdn.make_qk_norm_params(B=1, T=8, Hq=2, Hk=2, D=8, io_dtype="fp32", cu_seqlens=cu),
+              lambda p: osdn.osdn_qk_norm_fwd(p, q, q, None, None, None, None, yq, yk))]
+    for p, call in calls:
+        call(p)
+        p._cu_seqlens = cu.cpu()
+        with pytest.raises(ValueError, match="cu_seqlens: not on the current CUDA device"):
+            call(p)
+        p._cu_seqlens = cu
+        call(p)
+        del p._cu_seqlens                 # a pointer set by hand
+        call(p)
+    torch.cuda.synchronize()
