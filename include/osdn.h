@@ -302,7 +302,8 @@ int osdn_workspace_region(const osdn_params* p, int need_bwd, const char* name, 
  *     undefined results, but no access leaves the tensors.
  *   - Inputs are never written.  Outputs may not overlap inputs or one another unless stated.
  *   - A workspace belongs to one call, or to one forward and its backward, at a time.
- *   - T >= 1, any number of channels >= 1 where nothing else is stated; B T <= 1e9 and B T C <= 2e10.
+ *   - T >= 1, any number of channels from 1 to 2^31 - 1024 where nothing else is stated; B T <= 1e9 and
+ *     B T C <= 2e10.
  * ------------------------------------------------------------------------------------------- */
 
 /*

@@ -479,31 +479,31 @@ int backward_rows(const ConvArgs& a, int N, int ctas)
 
 }  // namespace
 
-// out0[(m % C) W + m / C] = sum of column m < W C, out1[m - W C] the others': one block per 32 columns.
-__global__ void __launch_bounds__(512) sum_rows_kernel(const float* part, int G, int C, int W, int M, float* out0, float* out1)
+// Columns 32 blockIdx.x .. of row blockIdx.y of the [W + 1, C] sums, in 64-bit offsets: (W + 1) C passes 32 bits before C does.
+__global__ void __launch_bounds__(512) sum_rows_kernel(const float* part, int G, int C, int W, float* out0, float* out1)
 {
     pdl_wait();
     __shared__ float s[16][33];
-    const int m = blockIdx.x * 32 + threadIdx.x;
+    const int c = blockIdx.x * 32 + threadIdx.x, j = blockIdx.y;
     float v = 0.f;
-    if (m < M)
-        for (int g = threadIdx.y; g < G; g += 16) v += part[(size_t)g * M + m];
+    if (c < C)
+        for (int g = threadIdx.y; g < G; g += 16) v += part[((size_t)g * (W + 1) + j) * C + c];
     s[threadIdx.y][threadIdx.x] = v;
     __syncthreads();
-    if (threadIdx.y || m >= M) return;
+    if (threadIdx.y || c >= C) return;
     float sum = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum += s[r][threadIdx.x];
-    if (m < W * C) {
-        if (out0) out0[(size_t)(m % C) * W + m / C] = sum;
+    if (j < W) {
+        if (out0) out0[(size_t)c * W + j] = sum;
     } else if (out1) {
-        out1[m - W * C] = sum;
+        out1[c] = sum;
     }
 }
 
-bool launch_sum_rows(const float* part, int G, int C, int W, int M, float* out0, float* out1, cudaStream_t st)
+bool launch_sum_rows(const float* part, int G, int C, int W, float* out0, float* out1, cudaStream_t st)
 {
-    return launch_after(sum_rows_kernel, dim3(div_up(M, 32)), dim3(32, 16), 0, st, part, G, C, W, M, out0, out1);
+    return launch_after(sum_rows_kernel, dim3(div_up(C, 32), W + 1), dim3(32, 16), 0, st, part, G, C, W, out0, out1);
 }
 
 size_t conv_workspace(const osdn_conv_params& p)
@@ -561,7 +561,7 @@ int conv_backward(const osdn_conv_params& p, const void* x, const float* w, cons
             const int rows = backward_rows(a, N, BWD_CTAS<N>);
             if (!set_smem(kernel, smem) || !launch_after(kernel, dim3(div_up(p.C, 32 * N), rows), dim3(128), smem, st, a)) return -1;
             stage_mark(st, "conv_sums");
-            return launch_sum_rows(a.partial, rows, p.C, W, (W + 1) * p.C, dw, dbias, st) ? 2 : -1;
+            return launch_sum_rows(a.partial, rows, p.C, W, dw, dbias, st) ? 2 : -1;
         };
         return lane_channels(p) > 1 ? go(std::integral_constant<int, 8 / (int)sizeof(T)>{}) : go(std::integral_constant<int, 1>{});
     });

@@ -513,7 +513,7 @@ int qk_norm_backward(const osdn_qk_norm_params& p, const void* q, const void* k,
         if (!set_smem(kernel, smem) || !launch_after(kernel, dim3(blocks), dim3(256), smem, st, a)) return -1;
         if (!a.partial) return 1;
         stage_mark(st, "qk_norm_sums");
-        return launch_sum_rows(a.partial, blocks, p.D, 1, 2 * p.D, dqw, dkw, st) ? 2 : -1;
+        return launch_sum_rows(a.partial, blocks, p.D, 1, dqw, dkw, st) ? 2 : -1;
     });
     stage_end(st);
     return n;

@@ -254,9 +254,9 @@ int qk_norm_backward(const osdn_qk_norm_params& p, const void* q, const void* k,
                      float* dkw, void* ws, cudaStream_t st);
 size_t qk_norm_workspace(const osdn_qk_norm_params& p);
 
-// Sums of the rows of part [G, M], in a fixed order: column m goes to out0[(m % C) W + m / C] where m < W C, else to
-// out1[m - W C]; either may be NULL.
-bool launch_sum_rows(const float* part, int G, int C, int W, int M, float* out0, float* out1, cudaStream_t st);
+// Sums over the first axis of part [G, W + 1, C], in a fixed order: out0[c W + j] of rows j < W, out1[c] of the last; either may
+// be NULL.
+bool launch_sum_rows(const float* part, int G, int C, int W, float* out0, float* out1, cudaStream_t st);
 
 // Launch count of the calling thread's last call (osdn_last_launch_count).
 int& last_launches();

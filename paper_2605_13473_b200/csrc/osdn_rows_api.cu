@@ -14,12 +14,14 @@ bool aligned(const void* const* ptrs, int n)
     return true;
 }
 
+constexpr long long MAX_CHANNELS = (1ll << 31) - 1024;   // the kernels' channel blocks end below 2^31
+
 int validate_batch(int B, int T, long long C, int io, int nseq, const int32_t* cu)
 {
     if (io != OSDN_FP32 && io != OSDN_BF16) return OSDN_INVALID_ARG;
     if (B <= 0 || nseq < 0) return OSDN_INVALID_ARG;
     if (nseq > 0 && (B != 1 || !cu)) return OSDN_INVALID_ARG;
-    if (T <= 0 || C <= 0) return OSDN_UNSUPPORTED_SHAPE;
+    if (T <= 0 || C <= 0 || C > MAX_CHANNELS) return OSDN_UNSUPPORTED_SHAPE;
     const double tokens = (double)B * T;
     if (tokens > 1.0e9 || tokens * (double)C > 2.0e10) return OSDN_UNSUPPORTED_SHAPE;
     if ((double)(nseq > 0 ? nseq : B) * (double)C > 2.0e10) return OSDN_UNSUPPORTED_SHAPE;

@@ -665,3 +665,24 @@ def test_a_sequence_of_nan_and_infinities_stays_alone(lens, bad):
         for k in (0, 1, 2, 5):
             m = keep if k in (0, 2) else others
             assert torch.equal(a[k][m], b[k][m]), (poison, k)
+
+
+def test_conv_weight_sums_past_32_bits():
+    """Channels times taps beyond 2^32: every channel's own gradient, exact for one token without activation."""
+    C, W = 859_000_064, 4
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x, dout = (torch.empty(1, C, device=DEV, dtype=torch.bfloat16).normal_(generator=g) for _ in range(2))
+    w = torch.empty(C, W, device=DEV)
+    w[:, :3], w[:, 3] = 1.0, dout[0]
+    p = osdn.make_conv_params(B=1, T=1, C=C, W=W, io_dtype="bf16", activation="none")
+    out, dx = torch.empty_like(x), torch.empty_like(x)
+    dw, db = torch.full((C, W), MARK, device=DEV), torch.full((C,), MARK, device=DEV)
+    ws = torch.empty(osdn.osdn_short_conv_workspace_bytes(p), device=DEV, dtype=torch.uint8)
+    osdn.osdn_short_conv_fwd(p, x, w, None, None, out, None)
+    osdn.osdn_short_conv_bwd(p, x, w, None, None, dout, None, dx, dw, db, None, ws)
+    for at in range(0, C, 1 << 27):                           # products of two bf16 values are fp32 values
+        part = slice(at, min(at + (1 << 27), C))
+        prod = x[0, part].float() * dout[0, part].float()
+        assert torch.equal(dw[part, 3], prod) and torch.equal(out[0, part], prod.bfloat16())
+        assert not bool(dw[part, :3].any()) and torch.equal(db[part], dout[0, part].float())
+        assert torch.equal(dx[0, part], dout[0, part].float().square().bfloat16())

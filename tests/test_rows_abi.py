@@ -272,3 +272,13 @@ def test_boundaries_elsewhere_are_refused():
         del p._cu_seqlens                 # a pointer set by hand
         call(p)
     torch.cuda.synchronize()
+
+
+def test_channels_up_to_where_their_blocks_stay_in_32_bits(lib):
+    most = 2 ** 31 - 1024
+    for make, ws, call, n in ((scan_params, lib.osdn_scan_workspace_bytes, lib.osdn_scan_step, 4),
+                              (conv_params, lib.osdn_short_conv_workspace_bytes, lib.osdn_short_conv_step, 5)):
+        for C in (most + 1, 2 ** 31 - 1):
+            p = make(B=1, T=1, C=C)
+            assert ws(ctypes.byref(p)) == 0 and call(ctypes.byref(p), *([FAKE] * n), NULL) == SHAPE
+        assert ws(ctypes.byref(make(B=1, T=1, C=most))) >= 4 * most
