@@ -312,7 +312,8 @@ int osdn_workspace_region(const osdn_params* p, int need_bwd, const char* name, 
  *     (OSDN_INPUT_COMPLEMENT, 1 - a_t without cancellation),   out_t = h_t.
  * Log gates are <= 0 and fp32, as everywhere in this library; -inf is a factor of zero.  All arithmetic is
  * fp32; a gate near one enters as its distance from one, so that memories of thousands of tokens keep
- * their length.
+ * their length.  A state (backward: its gradient) that becomes infinite or NaN stays one or the other in its
+ * channel to the end (beginning) of the sequence, behind gates of -inf too; an infinity may turn into NaN.
  */
 enum { OSDN_INPUT_PLAIN = 0, OSDN_INPUT_COMPLEMENT = 1 };
 typedef struct osdn_scan_params {

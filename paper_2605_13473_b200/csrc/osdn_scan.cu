@@ -1,4 +1,5 @@
 // Gated linear recurrence h_t = a_t h_{t-1} + b_t, a_t = exp(g_t), channel by channel: forward, backward, decode step.
+#include <cfloat>
 #include <cstddef>
 
 #include "osdn_rows.cuh"
@@ -320,13 +321,21 @@ template <typename V, bool FLAT, bool SPLIT> struct Stand {
     __device__ __forceinline__ int live(int t) const { return min(max(limit - t, 0), UNIT); }
 };
 
-// The map (g, b) of a stretch on the state in front of it; one in which a sequence begins (g = -inf) takes nothing from it.
+// The map (g, b) of a stretch on the state in front of it; one in which a sequence begins (g = -inf) takes nothing from it.  Gates
+// that add up to -inf are another thing, a factor of zero: a state that is not finite stays so behind it.
 template <int N> __device__ __forceinline__ F<N> apply(const F<N>& g, const F<N>& b, const F<N>& h)
 {
     const F<N> y = Decay<N>::of(g).step(h, b);
     F<N> r;
 #pragma unroll
     for (int k = 0; k < N; ++k) r.x[k] = g.x[k] == -INFINITY ? b.x[k] : y.x[k];
+    return r;
+}
+template <int N> __device__ __forceinline__ F<N> gate_sum(bool begins, const F<N>& sum)
+{
+    F<N> r;
+#pragma unroll
+    for (int k = 0; k < N; ++k) r.x[k] = begins ? -INFINITY : sum.x[k] == -INFINITY ? -FLT_MAX : sum.x[k];
     return r;
 }
 
@@ -351,6 +360,7 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
         copies_end();
     };
     F<N> mg = all<N>(0.f), mb = mg;
+    bool begins = false;   // a sequence, among these rows (REVERSE: ends)
     Marks marks;
     if (V::STAGED)
         for (int i = 0; i < V::DEPTH; ++i) ask(i, i);
@@ -407,10 +417,10 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
                 mb = REVERSE ? d.times(add(y, mb)) : d.step(mb, COMP ? mul(d.complement(), y) : y);
                 if (REVERSE && j && (marks.first >> j & 1)) q = previous(a, q);
             }
-            mg = all<N>(-INFINITY);
+            begins = true;
         }
     }
-    write<N>(&hand.g[at.warp][l], mg);
+    write<N>(&hand.g[at.warp][l], gate_sum<N>(begins, mg));
     write<N>(&hand.b[at.warp][l], mb);
     __syncthreads();
     if (at.warp == 0) {
@@ -418,10 +428,9 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
 #pragma unroll
         for (int k = 0; k < V::WARPS; ++k) {
             const int w = REVERSE ? V::WARPS - 1 - k : k;
-            const F<N> wg = read<N>(&hand.g[w][l]), sum = add(g, wg);
+            const F<N> wg = read<N>(&hand.g[w][l]);
             b = apply<N>(wg, read<N>(&hand.b[w][l]), b);
-#pragma unroll
-            for (int k = 0; k < N; ++k) g.x[k] = wg.x[k] == -INFINITY ? wg.x[k] : sum.x[k];
+            g = gate_sum<N>(g.x[0] == -INFINITY || wg.x[0] == -INFINITY, add(g, wg));   // all channels alike
         }
         write<N>(&hand.all_g[l], g);
         write<N>(&hand.all_b[l], b);

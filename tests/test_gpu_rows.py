@@ -686,3 +686,42 @@ def test_conv_weight_sums_past_32_bits():
         assert torch.equal(dw[part, 3], prod) and torch.equal(out[0, part], prod.bfloat16())
         assert not bool(dw[part, :3].any()) and torch.equal(db[part], dout[0, part].float())
         assert torch.equal(dx[0, part], dout[0, part].float().square().bfloat16())
+
+
+@pytest.mark.parametrize("comp", [False, True])
+@pytest.mark.parametrize("lens,dense,C", [([100], True, 64), ([20000], True, 64), ([300, 9000, 50], False, 64), ([2000], True, 5),
+                                          ([40] * 3, True, 64), ([9, 0, 30], False, 5)])
+def test_scan_state_that_is_not_finite_stays_so(comp, lens, dense, C):
+    """However a walk hands its state on: rows behind an infinity or NaN are not finite to the sequence's end, gates of -inf and
+    gates that add up to it in between or not; the rows in front, the other channels and the other sequences are as without."""
+    N, s = sum(lens), len(lens) - 1 if len(lens) < 3 else (1 if lens[1] else 2)
+    lo = sum(lens[:s])
+    hi = lo + lens[s]
+    x, gate = _scan_inputs(N, C, "fp32", 11, "edges")
+    gate[torch.rand(N, C, generator=_gen(12)) < 0.05] = -3e38
+    g = _gen(13)
+    dout, init, dfin = torch.randn(N, C, generator=g), torch.randn(len(lens), C, generator=g), torch.randn(len(lens), C, generator=g)
+    mid, ch = lo + lens[s] // 3, (torch.arange(C) % 2 == 0)
+    gate[mid, ch] = -0.5                                      # there the input reaches the state
+    gate[mid - 1, ch] = -0.5
+    want = _run_scan(x, gate, lens, dense, C, "fp32", comp, init, dout, dfin)
+    px, pd = x.clone(), dout.clone()
+    px[mid, ch] = torch.where(torch.arange(int(ch.sum())) % 3 == 0, float("nan"), float("inf"))
+    pd[mid, ch] = float("-inf")
+    rows = torch.arange(N)
+    behind, ahead = (rows >= mid) & (rows < hi), (rows <= mid) & (rows >= lo)
+    out, fin, _, _, _ = _run_scan(px, gate, lens, dense, C, "fp32", comp, init, dout, dfin)
+    hit = behind[:, None] & ch[None]
+    assert not bool(torch.isfinite(out.cpu()[hit]).any()) and not bool(torch.isfinite(fin.cpu()[s, ch]).any())
+    assert torch.equal(out.cpu()[~hit], want[0].cpu()[~hit])
+    _, _, dx, dg, dinit = _run_scan(x, gate, lens, dense, C, "fp32", comp, init, pd, dfin)
+    hit = ahead[:, None] & ch[None]
+    assert not bool(torch.isfinite(dg.cpu()[hit]).any()) and not bool(torch.isfinite(dinit.cpu()[s, ch]).any())
+    if not comp:
+        assert not bool(torch.isfinite(dx.cpu()[hit]).any())
+    assert torch.equal(dx.cpu()[~hit], want[2].cpu()[~hit]) and torch.equal(dg.cpu()[~hit], want[3].cpu()[~hit])
+    if dense and len(lens) == 1:                              # token by token
+        st, y = init.to(DEV), torch.empty(N, C, device=DEV)
+        p = osdn.make_scan_params(B=1, T=N, C=C, io_dtype="fp32", input_gate="complement" if comp else "plain")
+        osdn.osdn_scan_step(p, px.to(DEV), gate.to(DEV), st, y)
+        assert torch.equal(torch.isfinite(y), torch.isfinite(out)) and torch.equal(torch.isfinite(st), torch.isfinite(fin))
