@@ -78,8 +78,9 @@ def scan(x, g, lens, init, complement, dout=None, dfin=None):
     return got + [(dx, e_dx), (dg, e_dg), (dinit, e_dinit)]
 
 
-def conv(x, w, bias, lens, init, silu, quick, dout=None, dfin=None):
-    """x [N, C], w [C, W]; init, dfin [S, W-1, C] or None.  `quick`: the fast exponential and division (bf16)."""
+def conv(x, w, bias, lens, init, silu, quick, dout=None, dfin=None, chain=None):
+    """x [N, C], w [C, W]; init, dfin [S, W-1, C] or None.  `quick`: the fast exponential and division (bf16).  `chain`: additions
+    that a term of the weights' sums goes through at most (without it: any order of the N terms)."""
     x, w = x.double().cpu(), w.double().cpu()
     N, C = x.shape
     W, S = w.shape[1], len(lens)
@@ -136,12 +137,12 @@ def conv(x, w, bias, lens, init, silu, quick, dout=None, dfin=None):
     got = [(out, e_out), (final, torch.zeros_like(final))]
     if not grads:
         return got
-    terms = (N + 64) * U                        # a sum of N terms in any order
+    terms = (N + 64 if chain is None else chain) * U
     return got + [(dx, e_dx), (dw, e_dw + terms * m_dw), (db, e_db + terms * m_db), (dinit, e_dinit)]
 
 
-def norm(x, w, kind, eps, angle, layout, dy=None):
-    """x [N, H, D]; w [D] or None; angle [N, R/2] in fp64 or None.  Returns y (and dx, dw)."""
+def norm(x, w, kind, eps, angle, layout, dy=None, chain=None):
+    """x [N, H, D]; w [D] or None; angle [N, R/2] in fp64 or None.  Returns y (and dx, dw).  `chain`: as of conv, of the N H terms."""
     x = x.double().cpu()
     N, H, D = x.shape
     wt = torch.ones(D, dtype=torch.float64) if w is None else w.double().cpu()
@@ -176,7 +177,7 @@ def norm(x, w, kind, eps, angle, layout, dy=None):
     dx = r * (du - u * dot)
     e_dx = r * (e_du + u.abs() * e_dot + (E + 8 * U) * (du.abs() + u.abs() * m_dot))
     dw = (dv * u).sum((0, 1))
-    e_dw = (e_dv * u.abs()).sum((0, 1)) + (E + (N * H + 64) * U) * (dv * u).abs().sum((0, 1))
+    e_dw = (e_dv * u.abs()).sum((0, 1)) + (E + (N * H + 64 if chain is None else chain) * U) * (dv * u).abs().sum((0, 1))
     return [(y, ey), (dx, e_dx), (dw, e_dw)]
 
 
