@@ -55,18 +55,7 @@ __device__ __forceinline__ uint32_t pair_bf16(float a, float b)
 }
 template <int N> __device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&x)[N])
 {
-    if constexpr (N % 8 == 0) {
-#pragma unroll
-        for (int i = 0; i < N / 8; ++i) {
-            const uint4 v = reinterpret_cast<const uint4*>(p)[i];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 f = bf16_pair(w[j]);
-                x[8 * i + 2 * j] = f.x; x[8 * i + 2 * j + 1] = f.y;
-            }
-        }
-    } else if constexpr (N == 4) {
+    if constexpr (N == 4) {
         const uint2 v = *reinterpret_cast<const uint2*>(p);
         const float2 a = bf16_pair(v.x), b = bf16_pair(v.y);
         x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
@@ -88,12 +77,7 @@ template <int N> __device__ __forceinline__ void store_vec(float* p, const float
 }
 template <int N> __device__ __forceinline__ void store_vec(__nv_bfloat16* p, const float (&x)[N])
 {
-    if constexpr (N % 8 == 0) {
-#pragma unroll
-        for (int i = 0; i < N / 8; ++i)
-            reinterpret_cast<uint4*>(p)[i] = make_uint4(pair_bf16(x[8 * i], x[8 * i + 1]), pair_bf16(x[8 * i + 2], x[8 * i + 3]),
-                                                        pair_bf16(x[8 * i + 4], x[8 * i + 5]), pair_bf16(x[8 * i + 6], x[8 * i + 7]));
-    } else if constexpr (N == 4) {
+    if constexpr (N == 4) {
         *reinterpret_cast<uint2*>(p) = make_uint2(pair_bf16(x[0], x[1]), pair_bf16(x[2], x[3]));
     } else {
 #pragma unroll
