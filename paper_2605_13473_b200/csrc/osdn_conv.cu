@@ -486,8 +486,17 @@ __global__ void __launch_bounds__(512) sum_rows_kernel(const float* part, int G,
     __shared__ float s[16][33];
     const int c = blockIdx.x * 32 + threadIdx.x, j = blockIdx.y;
     float v = 0.f;
-    if (c < C)
-        for (int g = threadIdx.y; g < G; g += 16) v += part[((size_t)g * (W + 1) + j) * C + c];
+    if (c < C) {
+        const size_t row = (size_t)(W + 1) * C;
+        const float* p = part + threadIdx.y * row + (size_t)j * C + c;
+        for (int g = threadIdx.y; g < G; g += 8 * 16, p += 8 * 16 * row) {   // eight loads on their way, added in order
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = g + 16 * i < G ? p[16 * i * row] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += x[i];
+        }
+    }
     s[threadIdx.y][threadIdx.x] = v;
     __syncthreads();
     if (threadIdx.y || c >= C) return;
