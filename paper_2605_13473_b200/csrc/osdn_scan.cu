@@ -387,10 +387,9 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
             for (int j = 0; j < UNIT; j += SIDE) {
                 F<N> g[SIDE];
 #pragma unroll
-                for (int i = 0; i < SIDE; ++i) {
-                    g[i] = fg.r[j + i].get();
-                    mg = add(mg, g[i]);
-                }
+                for (int i = 0; i < SIDE; ++i) g[i] = fg.r[j + i].get();
+                mg = add(mg, add(add(g[0], g[1]), add(g[2], g[3])));   // equal gates lose the same way at every addition to a long sum
+                static_assert(SIDE == 4, "rows of one addition");
                 Decay<N>::template of<SIDE>(g, d + j);
 #pragma unroll
                 for (int i = j; i < j + SIDE; ++i) b[i] = COMP && !REVERSE ? mul(d[i].complement(), fx.r[i].get()) : fx.r[i].get();

@@ -1,5 +1,8 @@
 """The operators on rows of channels at sizes whose kernels and branches only larger batches reach: chunks of more than eight rows
 and several to a warp (convolution), whole tokens to a lane group (norms), sixteen warps (recurrence)."""
+import math
+
+import numpy as np
 import pytest
 import torch
 
@@ -155,3 +158,31 @@ def test_scan_backward_with_kept_and_recomputed_states_is_the_same(lens, dense, 
     a = _run_scan(x, gate, lens, dense, C, "bf16", True, init, dout, dfin)
     b = _run_scan(x, gate, lens, dense, C, "bf16", True, init, dout, dfin, saved=False)
     assert all(map(torch.equal, a, b))
+
+
+@pytest.mark.parametrize("T,B", [(131072, 1), (2048, 128)])
+def test_scan_of_equal_gates_rounds_as_its_rows_do(T, B):
+    """A gate of -1e-4 at every row.  A row's rounding, 2^-24 of the state at most and of either sign, is remembered for 10^4 rows:
+    2^-24 (1 - a^2)^-1/2 = 2^-24 sqrt(5000) in all, however a walk is split; twice that for a product of two states."""
+    C, rate = 8, 1e-4
+    g = _gen(1)
+    x, dout = 0.5 + torch.randn(T, C, generator=g), 0.5 + torch.randn(T, C, generator=g)
+    gate = torch.full((T, C), -rate)
+    many = lambda t: t.repeat(B, 1)  # noqa: E731
+    got = _run_scan(many(x), many(gate), [T] * B, True, C, "fp32", False, None, many(dout), None)
+    a = math.exp(float(gate[0, 0]))
+    xs, ds = x.double().numpy(), dout.double().numpy()
+    h, e, before, dh = np.zeros(C), np.zeros(C), np.empty((T, C)), np.empty((T, C))
+    for t in range(T):
+        before[t] = h
+        h = a * h + xs[t]
+    for t in range(T - 1, -1, -1):
+        dh[t] = ds[t] + e
+        e = a * dh[t]
+    out = np.concatenate([before[1:], h[None]])
+    room = 2.0 ** -24 * (2 * rate) ** -0.5
+    for name, y, want, r in zip(("out", "final", "dx", "dgate", "dinit"), got, (out, h[None], dh, before * (a * dh), e[None]),
+                                (room, room, room, 2 * room, room)):
+        y = y.double().cpu().view(B, -1, C)[B - 1].numpy()
+        off = np.linalg.norm(y - want) / np.linalg.norm(want)
+        assert off <= r, (name, off, r)
