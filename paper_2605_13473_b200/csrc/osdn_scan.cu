@@ -424,14 +424,16 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
     __syncthreads();
     if (at.warp == 0) {
         F<N> g = all<N>(0.f), b = g;
+        begins = false;
 #pragma unroll
         for (int k = 0; k < V::WARPS; ++k) {
             const int w = REVERSE ? V::WARPS - 1 - k : k;
             const F<N> wg = read<N>(&hand.g[w][l]);
             b = apply<N>(wg, read<N>(&hand.b[w][l]), b);
-            g = gate_sum<N>(g.x[0] == -INFINITY || wg.x[0] == -INFINITY, add(g, wg));   // all channels alike
+            g = add(g, wg);
+            begins |= wg.x[0] == -INFINITY;   // of all channels alike
         }
-        write<N>(&hand.all_g[l], g);
+        write<N>(&hand.all_g[l], gate_sum<N>(begins, g));
         write<N>(&hand.all_b[l], b);
     }
     cluster_arrive();
