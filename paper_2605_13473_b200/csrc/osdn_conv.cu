@@ -14,8 +14,8 @@ struct ConvArgs {
     long long walks;        // chunks of the whole batch
 };
 
-// z sigmoid(z) needs 1 / (1 + exp(-z)).  Where results are rounded to bf16 (2^-9 of the value) the hardware's exponential and
-// reciprocal (about 2^-21) are exact enough.
+// z sigmoid(z) needs 1 / (1 + exp(-z)).  Where results are rounded to bf16 (2^-8 of the value) the hardware's exponential and
+// reciprocal (about 2^-21, and 1.25 |z| 2^-24 by the argument) are exact enough; the weights' fp32 sums take them too.
 template <typename T, int L> __device__ __forceinline__ F<L> sigmoid(const F<L>& z)
 {
     F<L> s;

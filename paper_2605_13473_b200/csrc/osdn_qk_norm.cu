@@ -204,7 +204,8 @@ __global__ void __launch_bounds__(256) qk_norm_fwd_parts_kernel(NormArgs a)
 }
 
 // Many tokens: a lane group takes whole ones, whose angles serve all their heads.  Four heads' loads on their way in registers
-// (through shared memory, as the backward has it, 4 x 4096 tokens of 32 heads took 53 us instead of 49).
+// (through shared memory, as the backward has it, 4 x 4096 tokens of 32 heads took 8 % longer).  55 us there with rotated halves,
+// 74 % of the bytes' rate, and 47 with interleaved pairs: bound by the latency of the loads and of the halves' shuffles.
 template <typename T, int LH, int ROT, bool WEIGHTS>
 __global__ void __launch_bounds__(256, 4) qk_norm_fwd_kernel(NormArgs a)
 {
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(256, 4) qk_norm_fwd_kernel(NormArgs a)
 
 // What a lane reads of the heads of its tokens (one every `stride`), queries before keys, TENSORS of them side by side: copied
 // to the lane's own places of shared memory DEPTH heads ahead, since the arithmetic of a head is short against memory's latency
-// (backward of 4 x 4096 tokens, 32 rotated heads: with loads to registers, two heads at a time, 97 us, so 68).
+// (backward of 4 x 4096 tokens, 32 rotated heads: with loads to registers, two heads at a time, 97 us, so 67).
 template <typename T, int TENSORS, int DEPTH_> struct Ahead {
     static constexpr int DEPTH = DEPTH_, PIECES = (int)sizeof(T) / 2;   // of 16 bytes: eight features
     const T *q[TENSORS], *k[TENSORS], *src[TENSORS];

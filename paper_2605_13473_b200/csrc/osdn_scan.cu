@@ -13,7 +13,8 @@ constexpr int UNIT = 8;
 
 // exp(g) for g <= 0 as the sum of two floats, hi the nearest one to it:
 //   |g| <= 1/4:  from expm1(g) by its Taylor series to g^6 (remainder below 5e-8 of it): the sum keeps the distance from one;
-//   else:        hi alone, by the hardware's exponential (2^-22 of a; a <= 0.78 forgets it within a few tokens); -inf is zero.
+//   else:        hi alone, by the hardware's exponential: 2^-22 of a, and 1.25 |g| 2^-24 by the rounding of g log2(e) (g = -20:
+//                2^-20; a is 2e-9 there).  a <= 0.78 forgets either within a few tokens; -inf is zero.
 // As one rounded factor, a gate of -3e-4 keeps 1 - a to 1e-4 only, and a product of thousands of them drifts.  Two floats cost
 // one packed fma more a step and no selection (with the form chosen at every step 38 instructions an element instead of 29).
 template <int N> struct Decay {
@@ -451,10 +452,10 @@ __device__ __forceinline__ F<V::VEC> state_in_front(const ScanArgs& a, const S& 
 // state behind them on to the next warp before it does anything else, and walks the rows a second time from registers.  So
 // the only thing done one after another is a step of two fmas a unit, from warp to warp by named barriers.  With barriers of
 // all warps instead, tile by tile, the warps waited more than they worked (8 x 2048 tokens, 1024 channels, bf16: 38 to 51 us;
-// so 27.3, 4.9 TB/s of what has to be read and written, and the backward 41.5, 5.7 TB/s).  29 instructions an element, of which
-// the factor takes nine; bound by their issue and latency in bf16, by memory in fp32 (5.9 TB/s).
+// so 27.3, 4.9 TB/s of what has to be read and written, and the backward 41.3, 5.7 TB/s).  28 instructions an element, of which
+// the factor takes nine; bound by their issue and latency in bf16, by memory in fp32 (34.2 us, 5.9 TB/s; backward 57.8, 5.8).
 // Few walks are split among the warps of a cluster's CTAs, a stretch of rows to each, read once more for the state in front of
-// it: then nothing is waited for but rows (131072 tokens, 1024 channels: 415 us, 39 % of the bytes' rate; by the relay 490).
+// it: then nothing is waited for but rows (131072 tokens, 1024 channels: 414 us, 39 % of the bytes' rate; by the relay 490).
 // Rows that are all there and begin and end no sequence take the code without tests.
 // out == nullptr: only the states are kept.
 template <typename V, bool COMP, bool FLAT, bool SPLIT>
@@ -791,8 +792,9 @@ ScanArgs make_args(const osdn_scan_params& p)
 }
 
 // CTAs of a walk.  One, where walks alone give four of five SMs a CTA; else the walk is split, though its CTAs then read their
-// rows twice, until there are CTAs for four of five SMs, or for all of them twice over where every warp has many units (one
-// prompt of 2048 tokens, 1024 channels, forward: 13.8 us with eight CTAs to a walk, 16.3 with sixteen; 131072 tokens 614 and 551).
+// rows twice, until there are CTAs for four of five SMs, or for all of them twice over where every warp has many units.  1024
+// channels (16 walks), forward / backward with 4, 8 and 16 CTAs to a walk: one prompt of 2048 tokens 14.3 / 16.3, 13.8 / 15.6 and
+// 18.9 / 21.2 us (unsplit 25.1 / 29.8); 131072 tokens 503 / 579, 522 / 661 and 414 / 524 (unsplit 1438 / 1758).
 int span_of(long long walks, int units, int warps)
 {
     int span = 1;
@@ -801,9 +803,12 @@ int span_of(long long walks, int units, int warps)
     return span;
 }
 
-// Warps of a CTA.  Sixteen where an SM has one CTA with enough units for them, eight where it has two or the walk is short
-// (forward, 1024 channels, sixteen and eight: 8 x 2048 tokens 28.7 and 29.4 us, backward 40.9 and 52.1; 32 x 2048 106 and
-// 97; 64 x 100 23.5 and 15.4; one of 2048 22.0 and 15.7).
+// Warps of a CTA.  Sixteen where an SM has one CTA with enough units for them, eight where it has two or the walk is short.
+// 1024 channels, forward / backward with sixteen and with eight: 8 x 2048 tokens (128 walks) 27.3 / 41.1 and 28.4 / 46.9 us; 9 x 2048
+// 28.7 / 49.0 and 29.5 / 49.5; 16 x 2048 (256 walks) 53.0 / 80.2 and 47.4 / 91.1; 32 x 2048 105 / 159 and 92.7 / 168; 64 x 100 23.7 / 27.1
+// and 15.5 / 22.6; one of 2048, split over eight CTAs, 19.8 / 22.8 and 13.8 / 15.6; 131072 over sixteen 416 / 529 and 417 / 567.
+// From 149 walks on sixteen warps need a second wave, and eight would be the faster up to the line at 240 as well (10 x 2048 51.7 / 70.1
+// and 46.1 / 63.6; 12 x 2048 52.1 / 68.4 and 46.4 / 66.0; 14 x 2048 52.7 / 82.1 and 46.7 / 76.0; in fp32 66.3 / 102 and 66.2 / 110).
 struct Shape {
     int warps;
     bool split;
